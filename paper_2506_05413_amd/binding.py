@@ -1,6 +1,7 @@
 """Binding of libsmoothrot.so -- argument marshalling only.
 
-Function names and argument order follow include/smoothrot.h.  torch supplies
+Function names and argument order follow include/smoothrot.h and
+include/smoothrot_attention.h.  torch supplies
 device memory and the current stream; every step of the computation runs in the
 library's HIP kernels.  The per-token calls marshal their tensors in native code
 (csrc/marshal.cpp), which is built for one Python and one torch; the offline ones
@@ -17,6 +18,8 @@ import torch
 SR_OK, SR_ERR_NULL, SR_ERR_SHAPE, SR_ERR_UNSUPPORTED_K = 0, 1, 2, 3
 SR_ERR_ALIGN, SR_ERR_ARG, SR_ERR_WORKSPACE, SR_ERR_DEVICE = 4, 5, 6, 7
 SR_F16, SR_I32 = 0, 1
+SR_KV_F16, SR_KV_I4 = 0, 1
+SR_ROPE_PAIRS, SR_ROPE_HADAMARD = 1, 2
 SR_TUNE_GEMM_TILE, SR_TUNE_GEMM_GRID, SR_TUNE_GEMM_XCDM, SR_TUNE_DECODE_KERNEL = 0, 1, 2, 3
 SR_TUNE_FWHT4096, SR_TUNE_FWHT_STREAM, SR_TUNE_GEMM_WARM, SR_TUNE_CLIP_SEARCH = 4, 5, 6, 7
 SR_TUNE_KNOBS = 8
@@ -62,6 +65,23 @@ _SIGNATURES = {
     "sr_w4a4_linear_decode": (_int, [_vp, _i64, _i64, _i64, _vp, _f32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]),
 }
 
+
+# include/smoothrot_attention.h
+_ATTENTION_SIGNATURES = {
+    "sr_rope_kv_append": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _int, _f32, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "sr_kv_gather": (_int, [_vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "sr_attn_decode_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i64, _i64]),
+    "sr_attn_decode": (_int, [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _f32, _vp, _i64, _vp, _sz, _vp]),
+    "sr_attn_prefill": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _int, _f32, _vp, _i64, _vp]),
+}
+
+
+class sr_kv_cache(ctypes.Structure):
+    """sr_kv_cache of include/smoothrot_attention.h, for callers of raw()."""
+    _fields_ = [("K", _vp), ("V", _vp), ("K_params", _vp), ("V_params", _vp), ("n_pages", _i64), ("page_size", _i64),
+                ("n_kv_heads", _i64), ("head_dim", _i64), ("type", _int)]
+
+
 _lib = None
 
 
@@ -80,7 +100,7 @@ def raw() -> ctypes.CDLL:
             raise ImportError("libsmoothrot.so is not built: run `python -m paper_2506_05413_amd.build` "
                               "(there is no fallback path)")
         lib = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in _SIGNATURES.items():
+        for name, (res, args) in {**_SIGNATURES, **_ATTENTION_SIGNATURES}.items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = res, args
         _lib = lib
@@ -249,6 +269,41 @@ def sr_kv_quant_asym(X, group: int = 128, clip: float = 0.95, Q=None, scale=None
     """X fp16 [rows, D] -> (Q uint8 [rows, D/2], scale fp32 [rows, D/group], zero fp32 [rows, D/group])."""
     out = (_native or _marshal()).kv_quant_asym(X, group, clip, Q, scale, zero)
     return out if type(out) is tuple else _refused(out, "sr_kv_quant_asym")
+
+
+def sr_rope_kv_append(Q, K, V, positions, slots, cos_sin, cache, hadamard: bool = False, pairs: bool = False,
+                      clip: float = 0.95, Q_out=None, K_out=None):
+    """Q fp16 [T, n_heads * head_dim] (or None), K, V fp16 [T, n_kv_heads * head_dim], positions int32 [T], slots int64 [T],
+    cos_sin fp32 [max_pos, head_dim] (or None: no rotation, positions not looked at) -> turned queries Q_out.  The turned keys
+    and the values go into `cache`, a tuple (K, V, K_params, V_params) of contiguous tensors: fp16 [n_pages, n_kv_heads,
+    page_size, head_dim] and None, or uint8 [.., head_dim / 2] and fp32 [.., 2].  K_out: also receives the turned keys."""
+    out = (_native or _marshal()).rope_kv_append(Q, K, V, positions, slots, cos_sin, cache, hadamard, pairs, clip, Q_out, K_out)
+    return _refused(out, "sr_rope_kv_append") if type(out) is int else out
+
+
+def sr_kv_gather(slots, cache, K_out=None, V_out=None):
+    """slots int64 [T], cache as in sr_rope_kv_append -> (K, V) fp16 [T, n_kv_heads * head_dim]."""
+    out = (_native or _marshal()).kv_gather(slots, cache, K_out, V_out)
+    return out if type(out) is tuple else _refused(out, "sr_kv_gather")
+
+
+def sr_attn_decode_workspace_bytes(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, max_pages: int, page_size: int) -> int:
+    return int(raw().sr_attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim, max_pages, page_size))
+
+
+def sr_attn_decode(Q, cache, page_table, seq_lens, scale=None, O=None, workspace=None):
+    """Q fp16 [n_seqs, n_heads * head_dim], cache as in sr_rope_kv_append, page_table int32 [n_seqs, max_pages], seq_lens int32
+    [n_seqs] -> O fp16 like Q.  scale: 1 / sqrt(head_dim) if None.  workspace: a uint8 device tensor of
+    sr_attn_decode_workspace_bytes(...) bytes (reuse it from call to call); one is made per call if none is given."""
+    out = (_native or _marshal()).attn_decode(Q, cache, page_table, seq_lens, scale, O, workspace)
+    return _refused(out, "sr_attn_decode") if type(out) is int else out
+
+
+def sr_attn_prefill(Q, K, V, cu_q, cu_k, head_dim: int, causal: bool = True, scale=None, O=None):
+    """Q fp16 [T_q, n_heads * head_dim], K, V fp16 [T_k, n_kv_heads * head_dim], cu_q, cu_k int32 [n_seqs + 1] -> O fp16 like Q.
+    scale: 1 / sqrt(head_dim) if None."""
+    out = (_native or _marshal()).attn_prefill(Q, K, V, cu_q, cu_k, head_dim, causal, scale, O)
+    return _refused(out, "sr_attn_prefill") if type(out) is int else out
 
 
 def sr_linear_decode_workspace_bytes(M: int, K: int) -> int:

@@ -1,4 +1,4 @@
-// Argument marshalling of the per-token calls in native code: torch tensors in, the C ABI of include/smoothrot.h called
+// Argument marshalling of the per-token calls in native code: torch tensors in, the C ABI of include/ called
 // on the current stream, tensors out.  No computation here.
 //
 // Why: a decode step's kernels run 5 - 10 us each, and marshalling through Python and ctypes cost 8.5 - 15 us per call
@@ -13,12 +13,15 @@
 
 #include <ATen/ATen.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/smoothrot.h"
+#include "../../include/smoothrot_attention.h"
 
+#include <cmath>
 #include <exception>
 
 namespace {
@@ -299,12 +302,188 @@ PyObject *kv_quant_asym(PyObject *const *a)
                   : Py_BuildValue("(NNN)", THPVariable_Wrap(Q), THPVariable_Wrap(scale), THPVariable_Wrap(zero));
 }
 
+// ---- paged cache and attention: every tensor on the device that is current, sizes that follow from each other checked here ----
+
+const at::Tensor &here(const at::Tensor &t, const char *name)
+{
+    if (t.device().index() != c10::hip::current_device()) value_error("%s is not on the current device", name);
+    return t;
+}
+// rows of heads, [tokens, columns]
+const at::Tensor &rows_of(PyObject *o, const char *name, int64_t tokens, int64_t columns)
+{
+    const at::Tensor &t = here(matrix(o, at::kHalf, name), name);
+    if ((tokens >= 0 && t.size(0) != tokens) || (columns >= 0 && t.size(1) != columns)) value_error("%s has the wrong shape", name);
+    return t;
+}
+at::Tensor rows_out(PyObject *o, const char *name, int64_t tokens, int64_t columns, const at::Tensor &like)
+{
+    return o == Py_None ? empty({tokens, columns}, at::kHalf, like) : rows_of(o, name, tokens, columns);
+}
+// a vector of whole numbers, [n] (n < 0: any)
+const at::Tensor &indices(PyObject *o, const char *name, at::ScalarType type, int64_t n)
+{
+    const at::Tensor &t = tensor(o, name);
+    if (!t.is_cuda()) value_error("%s must be a device tensor", name);
+    here(t, name);
+    if (t.scalar_type() != type) value_error("%s must have dtype torch.%s", name, type == at::kInt ? "int32" : "int64");
+    if (t.dim() != 1 || (n >= 0 && t.size(0) != n) || (t.numel() > 1 && t.stride(0) != 1)) value_error("%s has the wrong shape", name);
+    return t;
+}
+template <typename T> T *at_of(const at::Tensor &t) { return static_cast<T *>(t.data_ptr()); }
+
+// (K, V, K_params, V_params): [pages, heads, page, head_dim] fp16, or uint8 with half as many columns and params [.., 2]
+sr_kv_cache cache_of(PyObject *o)
+{
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) {
+        PyErr_SetString(PyExc_TypeError, "cache must be a tuple (K, V, K_params, V_params)");
+        throw Raised();
+    }
+    sr_kv_cache c = {};
+    const at::Tensor &K = tensor(PyTuple_GET_ITEM(o, 0), "cache K"), &V = tensor(PyTuple_GET_ITEM(o, 1), "cache V");
+    const bool i4 = K.scalar_type() == at::kByte;
+    if (!K.is_cuda() || !V.is_cuda()) value_error("%s must be device tensors", "cache K and V");
+    if (!i4 && K.scalar_type() != at::kHalf) value_error("%s must have dtype torch.float16 or torch.uint8", "cache K");
+    if (V.scalar_type() != K.scalar_type() || K.dim() != 4 || V.sizes() != K.sizes()) value_error("%s must have four dimensions and agree", "cache K and V");
+    if (!here(K, "cache K").is_contiguous() || !here(V, "cache V").is_contiguous()) value_error("%s must be contiguous", "cache K and V");
+    c.K = K.data_ptr(), c.V = V.data_ptr();
+    c.n_pages = K.size(0), c.n_kv_heads = K.size(1), c.page_size = K.size(2), c.head_dim = i4 ? 2 * K.size(3) : K.size(3);
+    c.type = i4 ? SR_KV_I4 : SR_KV_F16;
+    for (int side = 0; side < 2; ++side) {
+        PyObject *p = PyTuple_GET_ITEM(o, 2 + side);
+        if (!i4) {
+            if (p != Py_None) value_error("%s goes with 4-bit codes only", side ? "cache V_params" : "cache K_params");
+            continue;
+        }
+        const char *name = side ? "cache V_params" : "cache K_params";
+        const at::Tensor &t = here(device_tensor(p, at::kFloat, name), name);
+        if (t.dim() != 4 || t.size(0) != c.n_pages || t.size(1) != c.n_kv_heads || t.size(2) != c.page_size || t.size(3) != 2 || !t.is_contiguous())
+            value_error("%s has the wrong shape", name);
+        (side ? c.V_params : c.K_params) = floats(t);
+    }
+    return c;
+}
+
+// Q, K, V, positions, slots, cos_sin, cache, hadamard, pairs, clip, Q_out, K_out
+PyObject *rope_kv_append(PyObject *const *a)
+{
+    const sr_kv_cache c = cache_of(a[6]);
+    const at::Tensor &K = rows_of(a[1], "K", -1, c.n_kv_heads * c.head_dim);
+    const int64_t T = K.size(0);
+    const at::Tensor &V = rows_of(a[2], "V", T, K.size(1));
+    const bool any_q = a[0] != Py_None;
+    at::Tensor Q, Qo, Ko;
+    int64_t heads = 0;
+    if (any_q) {
+        Q = rows_of(a[0], "Q", T, -1);
+        if (c.head_dim <= 0 || Q.size(1) == 0 || Q.size(1) % c.head_dim) value_error("%s is not made of heads of the cache's size", "Q");
+        heads = Q.size(1) / c.head_dim;
+        Qo = rows_out(a[10], "Q_out", T, Q.size(1), Q);
+    }
+    if (a[11] != Py_None) Ko = rows_of(a[11], "K_out", T, K.size(1));
+    const int64_t *slots = at_of<int64_t>(indices(a[4], "slots", at::kLong, T));
+    const float *table = nullptr;
+    const int32_t *positions = nullptr;
+    int64_t max_pos = 0;
+    if (a[5] != Py_None) {
+        const at::Tensor &t = here(matrix(a[5], at::kFloat, "cos_sin"), "cos_sin");
+        if (t.size(1) != c.head_dim || !t.is_contiguous()) value_error("%s has the wrong shape", "cos_sin");
+        table = floats(t), max_pos = t.size(0);
+        positions = at_of<int32_t>(indices(a[3], "positions", at::kInt, T));
+    }
+    const int flags = (truth(a[8]) ? SR_ROPE_PAIRS : 0) | (truth(a[7]) ? SR_ROPE_HADAMARD : 0);
+    const float clip = real(a[9]);
+    const void *q = any_q ? Q.data_ptr() : nullptr, *k = K.data_ptr(), *v = V.data_ptr();
+    void *qo = any_q ? Qo.data_ptr() : nullptr, *ko = Ko.defined() ? Ko.data_ptr() : nullptr, *st = stream();
+    const int64_t ldq = any_q ? row_stride(Q) : 0, ldqo = any_q ? row_stride(Qo) : 0, ldk = row_stride(K), ldv = row_stride(V),
+                  ldko = Ko.defined() ? row_stride(Ko) : 0;
+    const int status = released([&] {
+        return sr_rope_kv_append(q, ldq, k, ldk, v, ldv, T, heads, positions, slots, table, max_pos, flags, clip, &c, qo, ldqo, ko, ldko, st);
+    });
+    if (status) return PyLong_FromLong(status);
+    if (any_q) return THPVariable_Wrap(Qo);
+    Py_RETURN_NONE;
+}
+
+// slots, cache, K_out, V_out
+PyObject *kv_gather(PyObject *const *a)
+{
+    const sr_kv_cache c = cache_of(a[1]);
+    const at::Tensor &S = indices(a[0], "slots", at::kLong, -1);
+    const int64_t T = S.size(0), columns = c.n_kv_heads * c.head_dim;
+    const at::Tensor Ko = rows_out(a[2], "K_out", T, columns, S), Vo = rows_out(a[3], "V_out", T, columns, S);
+    const int64_t *slots = at_of<int64_t>(S);
+    void *k = Ko.data_ptr(), *v = Vo.data_ptr(), *st = stream();
+    const int64_t ldk = row_stride(Ko), ldv = row_stride(Vo);
+    const int status = released([&] { return sr_kv_gather(slots, T, &c, k, ldk, v, ldv, st); });
+    return status ? PyLong_FromLong(status) : pair(Ko, Vo);
+}
+
+// Q, cache, page_table, seq_lens, scale (None: 1 / sqrt(head_dim)), O, workspace
+PyObject *attn_decode(PyObject *const *a)
+{
+    const sr_kv_cache c = cache_of(a[1]);
+    const at::Tensor &Q = rows_of(a[0], "Q", -1, -1);
+    const int64_t B = Q.size(0);
+    if (c.head_dim <= 0 || Q.size(1) == 0 || Q.size(1) % c.head_dim) value_error("%s is not made of heads of the cache's size", "Q");
+    const int64_t heads = Q.size(1) / c.head_dim;
+    const at::Tensor &table = tensor(a[2], "page_table");
+    if (!table.is_cuda()) value_error("%s must be a device tensor", "page_table");
+    if (here(table, "page_table").scalar_type() != at::kInt) value_error("%s must have dtype torch.int32", "page_table");
+    if (table.dim() != 2 || table.size(0) != B || (table.size(1) > 1 && table.stride(1) != 1)) value_error("%s has the wrong shape", "page_table");
+    const int64_t pages = table.size(1), ld_table = B > 1 ? table.stride(0) : pages;
+    const int32_t *lens = at_of<int32_t>(indices(a[3], "seq_lens", at::kInt, B)), *entries = at_of<int32_t>(table);
+    const float scale = a[4] == Py_None ? 1.f / std::sqrt((float)c.head_dim) : real(a[4]);
+    const at::Tensor O = rows_out(a[5], "O", B, Q.size(1), Q);
+    at::Tensor work;
+    if (a[6] != Py_None) {
+        work = here(tensor(a[6], "workspace"), "workspace");
+        if (!work.is_contiguous()) value_error("%s must be contiguous", "workspace");
+    } else if (const size_t need = sr_attn_decode_workspace_bytes(B, heads, c.n_kv_heads, c.head_dim, pages, c.page_size)) {
+        work = empty({(int64_t)need}, at::kByte, Q);
+    }
+    const void *q = Q.data_ptr();
+    void *o = O.data_ptr(), *scratch = work.defined() ? work.data_ptr() : nullptr, *st = stream();
+    const size_t scratch_bytes = work.defined() ? work.nbytes() : 0;
+    const int64_t ldq = row_stride(Q), ldo = row_stride(O);
+    const int status = released([&] {
+        return sr_attn_decode(q, ldq, B, heads, &c, entries, pages, ld_table, lens, scale, o, ldo, scratch, scratch_bytes, st);
+    });
+    return status ? PyLong_FromLong(status) : THPVariable_Wrap(O);
+}
+
+// Q, K, V, cu_q, cu_k, head_dim, causal, scale (None: 1 / sqrt(head_dim)), O
+PyObject *attn_prefill(PyObject *const *a)
+{
+    const int64_t d = integer(a[5]);
+    if (d <= 0) return PyLong_FromLong(SR_ERR_ARG);
+    const at::Tensor &Q = rows_of(a[0], "Q", -1, -1), &K = rows_of(a[1], "K", -1, -1), &V = rows_of(a[2], "V", K.size(0), K.size(1));
+    if (Q.size(1) == 0 || Q.size(1) % d || K.size(1) == 0 || K.size(1) % d) value_error("%s are not made of heads of head_dim", "Q and K");
+    const at::Tensor &cq = indices(a[3], "cu_q", at::kInt, -1);
+    if (cq.size(0) < 1) value_error("%s has the wrong shape", "cu_q");
+    const int64_t n = cq.size(0) - 1;
+    const at::Tensor &ck = indices(a[4], "cu_k", at::kInt, n + 1);
+    const int causal = truth(a[6]);
+    const float scale = a[7] == Py_None ? 1.f / std::sqrt((float)d) : real(a[7]);
+    const at::Tensor O = rows_out(a[8], "O", Q.size(0), Q.size(1), Q);
+    const void *q = Q.data_ptr(), *k = K.data_ptr(), *v = V.data_ptr();
+    const int32_t *cu_q = at_of<int32_t>(cq), *cu_k = at_of<int32_t>(ck);
+    void *o = O.data_ptr(), *st = stream();
+    const int64_t ldq = row_stride(Q), ldk = row_stride(K), ldv = row_stride(V), ldo = row_stride(O);
+    const int64_t Tq = Q.size(0), Tk = K.size(0), heads = Q.size(1) / d, kv = K.size(1) / d;
+    const int status = released([&] {
+        return sr_attn_prefill(q, ldq, k, ldk, v, ldv, cu_q, cu_k, n, Tq, Tk, heads, kv, d, causal, scale, o, ldo, st);
+    });
+    return status ? PyLong_FromLong(status) : THPVariable_Wrap(O);
+}
+
 PyObject *current_stream(PyObject *const *) { return PyLong_FromVoidPtr(stream()); }
 
 #define SR_ENTRY(F, N) {#F, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<F, N>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SR_ENTRY(fwht_quant_act, 5), SR_ENTRY(fwht_quant_act_heads, 7), SR_ENTRY(fwht_quant_act_f6, 6),
                          SR_ENTRY(swiglu_fwht_quant_act, 7), SR_ENTRY(w4a4_gemm, 7), SR_ENTRY(w4a4_gemm_f6, 10),
-                         SR_ENTRY(w4a4_linear_decode, 9), SR_ENTRY(kv_quant_asym, 6), SR_ENTRY(current_stream, 0), {nullptr, nullptr, 0, nullptr}};
+                         SR_ENTRY(w4a4_linear_decode, 9), SR_ENTRY(kv_quant_asym, 6), SR_ENTRY(rope_kv_append, 12), SR_ENTRY(kv_gather, 4),
+                         SR_ENTRY(attn_decode, 7), SR_ENTRY(attn_prefill, 9), SR_ENTRY(current_stream, 0), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

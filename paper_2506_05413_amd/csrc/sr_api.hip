@@ -1,6 +1,7 @@
 // C ABI of libsmoothrot: host-side argument validation and dispatch.
 // Every check happens before the first launch, so an error leaves all outputs untouched.
 #include "../../include/smoothrot.h"
+#include "../../include/smoothrot_attention.h"
 #include "sr_common.h"
 
 #include <atomic>
@@ -311,6 +312,119 @@ int sr_kv_quant_asym(const void *X_f16, int64_t rows, int64_t D, int64_t ldx, in
     if (ldx % 8 != 0 || !aligned16(X_f16) || !aligned16(Q)) return SR_ERR_ALIGN;
     return dev(sr::launch_kv_quant(X_f16, rows, D, ldx, group, clip, Q, scale, zero,
                                    static_cast<hipStream_t>(stream)));
+}
+
+// ---- paged cache and attention ----------------------------------------------------------------------------------------
+static bool head_dim_ok(int64_t d) { return d == 64 || d == 128; }
+
+static int check_cache(const sr_kv_cache *cache, sr::KvCache &c)
+{
+    if (!cache) return SR_ERR_NULL;
+    if (cache->type != SR_KV_F16 && cache->type != SR_KV_I4) return SR_ERR_ARG;
+    if (!head_dim_ok(cache->head_dim)) return SR_ERR_ARG;
+    if (!sr::is_pow2(cache->page_size) || cache->page_size < 16 || cache->page_size > (1 << 20)) return SR_ERR_ARG;
+    if (cache->n_pages < 1 || cache->n_pages >= ((int64_t)1 << 31) || cache->n_pages >= ((int64_t)1 << 40) / cache->page_size ||
+        cache->n_kv_heads < 1 || cache->n_kv_heads >= (1 << 20))
+        return SR_ERR_SHAPE;
+    c.i4 = cache->type == SR_KV_I4;
+    if (!cache->K || !cache->V || (c.i4 && (!cache->K_params || !cache->V_params))) return SR_ERR_NULL;
+    if (!aligned16(cache->K) || !aligned16(cache->V) || (c.i4 && (!aligned16(cache->K_params) || !aligned16(cache->V_params))))
+        return SR_ERR_ALIGN;
+    c.K = cache->K, c.V = cache->V, c.Kp = cache->K_params, c.Vp = cache->V_params;
+    c.pages = cache->n_pages, c.page_size = cache->page_size, c.heads = cache->n_kv_heads, c.dim = cache->head_dim;
+    return SR_OK;
+}
+static bool heads_fit(int64_t n_heads, int64_t n_kv_heads)
+{
+    return n_kv_heads >= 1 && n_heads >= n_kv_heads && n_heads < (1 << 20) && n_heads % n_kv_heads == 0;
+}
+static bool scale_ok(float scale) { return scale > 0.f && scale <= 3.4e38f; }
+
+int sr_rope_kv_append(const void *Q_f16, int64_t ldq, const void *K_f16, int64_t ldk, const void *V_f16, int64_t ldv,
+                      int64_t T, int64_t n_heads, const int32_t *positions, const int64_t *slots,
+                      const float *cos_sin, int64_t max_pos, int flags, float clip, const sr_kv_cache *cache,
+                      void *Q_out, int64_t ldqo, void *K_out, int64_t ldko, void *stream)
+{
+    sr::KvCache c;
+    if (const int e = check_cache(cache, c)) return e;
+    const int64_t dq = n_heads * c.dim, dk = c.heads * c.dim;
+    if (T < 0 || n_heads < 0 || n_heads >= (1 << 20) || ldk < dk || ldv < dk || (n_heads && (ldq < dq || ldqo < dq)) || (K_out && ldko < dk))
+        return SR_ERR_SHAPE;
+    if (T >= (1 << 27) || T * (n_heads + 2 * c.heads) >= (1 << 27)) return SR_ERR_SHAPE;
+    if (flags & ~(SR_ROPE_PAIRS | SR_ROPE_HADAMARD) || (c.i4 && !(clip > 0.f && clip <= 1.f))) return SR_ERR_ARG;
+    if (cos_sin && (max_pos < 1 || max_pos >= ((int64_t)1 << 31))) return SR_ERR_SHAPE;
+    if (T == 0) return SR_OK;
+    if (!K_f16 || !V_f16 || !slots || (cos_sin && !positions) || (n_heads && (!Q_f16 || !Q_out))) return SR_ERR_NULL;
+    if (ldk % 8 != 0 || ldv % 8 != 0 || !aligned16(K_f16) || !aligned16(V_f16) || (cos_sin && !aligned16(cos_sin)) ||
+        (n_heads && (ldq % 8 != 0 || ldqo % 8 != 0 || !aligned16(Q_f16) || !aligned16(Q_out))) ||
+        (K_out && (ldko % 8 != 0 || !aligned16(K_out))))
+        return SR_ERR_ALIGN;
+    return dev(sr::launch_rope_kv_append(Q_f16, ldq, K_f16, ldk, V_f16, ldv, T, n_heads, positions, slots, cos_sin, max_pos,
+                                         flags & SR_ROPE_PAIRS, flags & SR_ROPE_HADAMARD, clip, c, Q_out, ldqo, K_out, ldko,
+                                         static_cast<hipStream_t>(stream)));
+}
+
+int sr_kv_gather(const int64_t *slots, int64_t T, const sr_kv_cache *cache, void *K_out, int64_t ldko, void *V_out, int64_t ldvo,
+                 void *stream)
+{
+    sr::KvCache c;
+    if (const int e = check_cache(cache, c)) return e;
+    if (T < 0 || T >= (1 << 27) || T * 2 * c.heads >= (1 << 27) || ldko < c.heads * c.dim || ldvo < c.heads * c.dim) return SR_ERR_SHAPE;
+    if (T == 0) return SR_OK;
+    if (!slots || !K_out || !V_out) return SR_ERR_NULL;
+    if (ldko % 8 != 0 || ldvo % 8 != 0 || !aligned16(K_out) || !aligned16(V_out)) return SR_ERR_ALIGN;
+    return dev(sr::launch_kv_gather(slots, T, c, K_out, ldko, V_out, ldvo, static_cast<hipStream_t>(stream)));
+}
+
+static bool decode_shape_ok(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t max_pages, int64_t page_size)
+{
+    return n_seqs >= 0 && n_seqs < (1 << 20) && heads_fit(n_heads, n_kv_heads) && n_seqs * n_heads < (1 << 24) && max_pages >= 1 &&
+           page_size >= 16 && page_size <= (1 << 20) && max_pages <= (1 << 30) / page_size;
+}
+
+size_t sr_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int64_t max_pages,
+                                      int64_t page_size)
+{
+    if (n_seqs <= 0 || !head_dim_ok(head_dim) || !decode_shape_ok(n_seqs, n_heads, n_kv_heads, max_pages, page_size)) return 0;
+    return sr::attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim, max_pages * page_size);
+}
+
+int sr_attn_decode(const void *Q_f16, int64_t ldq, int64_t n_seqs, int64_t n_heads, const sr_kv_cache *cache,
+                   const int32_t *page_table, int64_t max_pages, int64_t ld_table, const int32_t *seq_lens, float scale,
+                   void *O_f16, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream)
+{
+    sr::KvCache c;
+    if (const int e = check_cache(cache, c)) return e;
+    if (!decode_shape_ok(n_seqs, n_heads, c.heads, max_pages, c.page_size)) return SR_ERR_SHAPE;
+    if (ldq < n_heads * c.dim || ldo < n_heads * c.dim || ld_table < max_pages) return SR_ERR_SHAPE;
+    if (!scale_ok(scale)) return SR_ERR_ARG;
+    if (n_seqs == 0) return SR_OK;
+    if (!Q_f16 || !page_table || !seq_lens || !O_f16) return SR_ERR_NULL;
+    if (ldq % 8 != 0 || ldo % 8 != 0 || !aligned16(Q_f16) || !aligned16(O_f16)) return SR_ERR_ALIGN;
+    const size_t need = sr::attn_decode_workspace_bytes(n_seqs, n_heads, c.heads, c.dim, max_pages * c.page_size);
+    if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return SR_ERR_WORKSPACE;
+    return dev(sr::launch_attn_decode(Q_f16, ldq, n_seqs, n_heads, c, page_table, max_pages, ld_table, seq_lens, scale, O_f16, ldo,
+                                      workspace, static_cast<hipStream_t>(stream)));
+}
+
+int sr_attn_prefill(const void *Q_f16, int64_t ldq, const void *K_f16, int64_t ldk, const void *V_f16, int64_t ldv,
+                    const int32_t *cu_q, const int32_t *cu_k, int64_t n_seqs, int64_t T_q, int64_t T_k,
+                    int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int causal, float scale,
+                    void *O_f16, int64_t ldo, void *stream)
+{
+    constexpr int64_t most = ((int64_t)1 << 31) - 1, stride = 1 << 23;
+    if (!head_dim_ok(head_dim) || !scale_ok(scale)) return SR_ERR_ARG;
+    if (n_seqs < 0 || n_seqs >= most || T_q < 0 || T_q > most || T_k < 0 || T_k > most || !heads_fit(n_heads, n_kv_heads)) return SR_ERR_SHAPE;
+    if (ldq < n_heads * head_dim || ldo < n_heads * head_dim || ldk < n_kv_heads * head_dim || ldv < n_kv_heads * head_dim) return SR_ERR_SHAPE;
+    if (ldq >= stride || ldk >= stride || ldv >= stride || ldo >= stride) return SR_ERR_SHAPE;
+    if (sr::attn_prefill_workgroups(T_q, n_seqs, n_heads) > most) return SR_ERR_SHAPE;
+    if (T_q == 0 || n_seqs == 0) return SR_OK;
+    if (!Q_f16 || !O_f16 || !cu_q || !cu_k || (T_k && (!K_f16 || !V_f16))) return SR_ERR_NULL;
+    if (ldq % 8 != 0 || ldk % 8 != 0 || ldv % 8 != 0 || ldo % 8 != 0 || !aligned16(Q_f16) || !aligned16(O_f16) ||
+        (T_k && (!aligned16(K_f16) || !aligned16(V_f16))))
+        return SR_ERR_ALIGN;
+    return dev(sr::launch_attn_prefill(Q_f16, ldq, K_f16, ldk, V_f16, ldv, cu_q, cu_k, n_seqs, T_q, T_k, n_heads, n_kv_heads, head_dim,
+                                       causal != 0, scale, O_f16, ldo, static_cast<hipStream_t>(stream)));
 }
 
 size_t sr_linear_decode_workspace_bytes(int64_t M, int64_t K) { return sr::linear_decode_workspace_bytes(M, K); }

@@ -1,5 +1,5 @@
 // Internal declarations shared by the HIP translation units of libsmoothrot.
-// (Public interface: include/smoothrot.h.)
+// (Public interface: include/smoothrot.h, include/smoothrot_attention.h.)
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -156,6 +156,34 @@ hipError_t launch_transpose_absmax_f16(const void *W_f16, int64_t K, int64_t N, 
 // asymmetric 4-bit group quantiser (keys / values)
 hipError_t launch_kv_quant(const void *X_f16, int64_t rows, int64_t D, int64_t ldx, int64_t group, float clip,
                            uint8_t *Q, float *scale, float *zero, hipStream_t st);
+
+// A paged cache of keys and values (sr_kv_cache of the public header, checked).
+struct KvCache {
+    void *K, *V;
+    float *Kp, *Vp;                                      // (scale, zero) per row of 4-bit codes
+    int64_t pages, page_size, heads, dim;
+    bool i4;
+};
+
+// rotation, quantiser and scatter of new tokens; rows of the cache back as fp16 (see kv_cache.hip)
+hipError_t launch_rope_kv_append(const void *Q, int64_t ldq, const void *K, int64_t ldk, const void *V, int64_t ldv, int64_t T,
+                                 int64_t n_heads, const int32_t *positions, const int64_t *slots, const float *cos_sin,
+                                 int64_t max_pos, bool pairs, bool had, float clip, const KvCache &c, void *Q_out, int64_t ldqo,
+                                 void *K_out, int64_t ldko, hipStream_t st);
+hipError_t launch_kv_gather(const int64_t *slots, int64_t T, const KvCache &c, void *K_out, int64_t ldko, void *V_out, int64_t ldvo,
+                            hipStream_t st);
+
+// attention of one token per sequence over the cache (see attn_decode.hip); max_len = tokens that the page table covers
+size_t attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t kv, int64_t dim, int64_t max_len);
+hipError_t launch_attn_decode(const void *Q, int64_t ldq, int64_t n_seqs, int64_t n_heads, const KvCache &c, const int32_t *table,
+                              int64_t max_pages, int64_t ld_table, const int32_t *lens, float scale, void *O, int64_t ldo,
+                              void *workspace, hipStream_t st);
+
+// attention of packed prompts (see attn_prefill.hip)
+int64_t attn_prefill_workgroups(int64_t T_q, int64_t n_seqs, int64_t n_heads);
+hipError_t launch_attn_prefill(const void *Q, int64_t ldq, const void *K, int64_t ldk, const void *V, int64_t ldv,
+                               const int32_t *cu_q, const int32_t *cu_k, int64_t n_seqs, int64_t T_q, int64_t T_k, int64_t n_heads,
+                               int64_t kv, int64_t dim, bool causal, float scale, void *O, int64_t ldo, hipStream_t st);
 
 // decode step behind one entry point: rotate + quantise up to 16 token rows and multiply (see linear_decode.hip).
 // workspace: linear_decode_workspace_bytes(M, K) bytes (0 = none needed).

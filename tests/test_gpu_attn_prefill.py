@@ -1,0 +1,145 @@
+"""sr_attn_prefill against 64-bit attention."""
+import numpy as np
+import pytest
+import torch
+
+from attention_bounds import attention_bound, check_attention
+from oracle import attention_oracle as ao
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def ends(lens):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+
+
+def make(nq, nk, H, KV, d, seed=0, spread=1.5):
+    rng = np.random.default_rng(seed)
+    q = (spread * rng.standard_normal((sum(nq), H, d))).astype(np.float16)
+    k, v = (rng.standard_normal((sum(nk), KV, d)).astype(np.float16) for _ in range(2))
+    return q, k, v
+
+
+def check(got, q, k, v, nq, nk, causal, scale, what=""):
+    """got [T, H, d] against every sequence and head."""
+    H, KV, d = q.shape[1], k.shape[1], q.shape[2]
+    i = j = 0
+    worst = 0.0
+    for s, (n, m) in enumerate(zip(nq, nk)):
+        seen = ao.causal(n, m) if causal else np.ones((n, m), bool)
+        for h in range(H if n else 0):
+            qq, kk, vv = q[i:i + n, h].astype(np.float64), k[j:j + m, h * KV // H].astype(np.float64), v[j:j + m, h * KV // H].astype(np.float64)
+            o, p, sc = ao.attend(qq, kk, vv, scale, seen)
+            bound = attention_bound(qq, np.abs(kk), vv, np.abs(vv), o, p, sc, scale)
+            worst = max(worst, check_attention(got[i:i + n, h], o, bound, "%s sequence %d (%d queries, %d keys) head %d" % (what, s, n, m, h)))
+        i, j = i + n, j + m
+    return worst
+
+
+def run(sr, q, k, v, nq, nk, causal=True, scale=None, **more):
+    T, H, d = q.shape
+    got = sr.sr_attn_prefill(dev(q.reshape(T, -1)), dev(k.reshape(len(k), -1)), dev(v.reshape(len(v), -1)), dev(ends(nq)), dev(ends(nk)), d, causal, scale, **more)
+    torch.cuda.synchronize()
+    return got.cpu().numpy().reshape(T, H, d)
+
+
+LENS = [1, 2, 31, 32, 33, 63, 64, 65, 0, 127, 128, 129, 200, 300]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,KV", [(8, 2), (3, 3), (5, 1)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed_lengths(gpu, d, H, KV, causal):
+    print("case prefill", d, H, KV, causal, flush=True)
+    q, k, v = make(LENS, LENS, H, KV, d, seed=d + H)
+    check(run(gpu, q, k, v, LENS, LENS, causal), q, k, v, LENS, LENS, causal, 1 / np.sqrt(d))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_other_numbers_of_keys(gpu, d, causal):
+    """Chunks behind a cached prefix, more queries than keys (rows that see nothing), no keys, no queries."""
+    nq = [1, 1, 40, 130, 7, 150, 33, 0, 64, 5]
+    nk = [1, 500, 40, 700, 0, 20, 97, 50, 63, 129]
+    q, k, v = make(nq, nk, 4, 2, d, seed=d)
+    got = run(gpu, q, k, v, nq, nk, causal)
+    check(got, q, k, v, nq, nk, causal, 1 / np.sqrt(d))
+    at = np.cumsum([0] + nq)
+    assert (got[at[4]:at[5]] == 0).all()
+    if causal:
+        assert (got[at[5]:at[5] + 130] == 0).all()
+
+
+@pytest.mark.parametrize("T,H,KV,d", [(1, 32, 8, 128), (1000, 4, 1, 128), (777, 2, 2, 64)])
+def test_one_prompt(gpu, T, H, KV, d):
+    q, k, v = make([T], [T], H, KV, d, seed=T)
+    check(run(gpu, q, k, v, [T], [T]), q, k, v, [T], [T], True, 1 / np.sqrt(d))
+
+
+@pytest.mark.parametrize("scale", [1e-4, 0.7, 4.0])
+def test_scales_from_flat_to_one_token(gpu, scale):
+    q, k, v = make([150, 90], [150, 90], 2, 1, 128)
+    check(run(gpu, q, k, v, [150, 90], [150, 90], scale=scale), q, k, v, [150, 90], [150, 90], True, float(np.float32(scale)))
+
+
+def test_scores_that_grow_and_fall_along_the_keys(gpu):
+    """The running maximum is replaced at every tile, and never."""
+    T, d = 400, 128
+    q, k, v = make([T], [T], 2, 2, d)
+    for sign in (1, -1):
+        kk = k.copy()
+        q[:, :, 0], kk[:, :, 0] = 8, (sign * np.linspace(-30, 30, T)[:, None]).astype(np.float16)
+        check(run(gpu, q, kk, v, [T], [T], False), q, kk, v, [T], [T], False, 1 / np.sqrt(d))
+
+
+def test_rows_of_no_sequence_and_other_columns_stay(gpu):
+    d, H, KV = 64, 3, 1
+    nq, nk = [50, 20], [50, 20]
+    q, k, v = make(nq, nk, H, KV, d)
+    pad = 13
+    fused = torch.full((70 + pad, (H + 2 * KV) * d + 16), float("nan"), dtype=torch.float16, device="cuda")
+    fused[:70, :H * d], fused[:70, H * d:H * d + d], fused[:70, H * d + d:H * d + 2 * d] = dev(q.reshape(70, -1)), dev(k.reshape(70, -1)), dev(v.reshape(70, -1))
+    out = torch.full((70 + pad, H * d + 16), 7.0, dtype=torch.float16, device="cuda")
+    gpu.sr_attn_prefill(fused[:, :H * d], fused[:, H * d:H * d + d], fused[:, H * d + d:H * d + 2 * d], dev(ends(nq)), dev(ends(nk)), d, O=out[:, 8:8 + H * d])
+    torch.cuda.synchronize()
+    check(out[:70, 8:8 + H * d].cpu().numpy().reshape(70, H, d), q, k, v, nq, nk, True, 1 / 8)
+    assert (out[70:] == 7).all() and (out[:, :8] == 7).all() and (out[:, 8 + H * d:] == 7).all()
+
+
+def test_neighbours_do_not_leak(gpu):
+    """A sequence of NaN and infinities between two others."""
+    nq = [70, 33, 90]
+    q, k, v = make(nq, nq, 2, 1, 128)
+    bad = slice(70, 103)
+    k[bad], v[bad], q[bad] = np.nan, np.inf, np.nan
+    got = run(gpu, q, k, v, nq, nq)
+    for part, n in ((slice(0, 70), 70), (slice(103, 193), 90)):
+        check(got[part], q[part], k[part], v[part], [n], [n], True, 1 / np.sqrt(128))
+
+
+def test_ends_that_do_not_fit_are_cut(gpu):
+    q, k, v = make([100], [100], 2, 1, 64)
+    want = run(gpu, q, k, v, [60, 40], [60, 40])
+    Q, K, V = dev(q.reshape(100, -1)), dev(k.reshape(100, -1)), dev(v.reshape(100, -1))
+    cu = dev(np.array([0, 60, 1000], np.int32))
+    got = gpu.sr_attn_prefill(Q, K, V, cu, cu, 64)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(got.cpu().numpy().reshape(want.shape), want)
+    # descending and negative ends: no rows
+    out = torch.full((100, 128), 7.0, dtype=torch.float16, device="cuda")
+    cu = dev(np.array([-5, -2, -9], np.int32))
+    gpu.sr_attn_prefill(Q, K, V, cu, cu, 64, O=out)
+    torch.cuda.synchronize()
+    assert (out == 7).all()
+
+
+def test_more_sequences_than_lanes(gpu):
+    rng = np.random.default_rng(6)
+    lens = [int(n) for n in rng.integers(0, 12, 300)]
+    lens[170] = 200
+    q, k, v = make(lens, lens, 2, 2, 64)
+    check(run(gpu, q, k, v, lens, lens), q, k, v, lens, lens, True, 1 / 8)
