@@ -44,8 +44,8 @@ typedef struct {
  *     y <- y H / sqrt(head_dim)                       SR_ROPE_HADAMARD: the transform inside the head on queries and keys
  *                                                     alike, which leaves q . k what it was (paper: head-wise online Hadamard)
  * in fp32 (every operation rounded), then rounded to fp16.  Values are not turned.  A 4-bit cache receives the codes of those
- * fp16 numbers under the formula of sr_kv_quant_asym with group = head_dim, quotients correctly rounded (so a code on a
- * rounding boundary may differ from sr_kv_quant_asym's).
+ * fp16 numbers under the formula of sr_kv_quant_asym with group = head_dim, d = (hi - lo) times the fp32 number nearest 1 / 15,
+ * quotients by d correctly rounded (so d may differ from sr_kv_quant_asym's by a rounding, and a code on a rounding boundary).
  *   Q_f16          fp16 [T, n_heads * head_dim], row stride ldq; may be NULL with n_heads = 0
  *   K_f16, V_f16   fp16 [T, n_kv_heads * head_dim], row strides ldk, ldv (e.g. columns of one fused projection)
  *   positions      int32 [T]; positions outside [0, max_pos) are taken as the nearest inside

@@ -53,7 +53,7 @@ def quantise_heads(v, clip=0.95, dtype=np.float64):
     v = np.asarray(v).astype(dtype)
     clip = dtype(np.float32(clip))
     hi, lo = clip * v.max(-1), clip * v.min(-1)
-    scale = np.where(hi == lo, dtype(1), (hi - lo) / dtype(15))
+    scale = np.where(hi == lo, dtype(1), (hi - lo) * dtype(1 / 15))
     zero = -np.rint(lo / scale)
     codes = np.clip(np.rint(v / scale[..., None]) + zero[..., None], 0, 15)
     return codes.astype(np.uint8), scale, zero

@@ -2,7 +2,7 @@
 //
 //   halves:  y_i = x_i cos_i - x_{i+D/2} sin_i,   y_{i+D/2} = x_{i+D/2} cos_i + x_i sin_i       (pairs: 2i and 2i + 1)
 //   Hadamard: y <- y H_D / sqrt(D) inside the head, butterflies over strides 1, 2, 4, ..
-//   4 bits, per token and head:  D = (hi - lo) / 15, z = -rint(lo / D), code = clamp(rint(v / D) + z, 0, 15)
+//   4 bits, per token and head:  D = (hi - lo) * (1 / 15), z = -rint(lo / D), code = clamp(rint(v / D) + z, 0, 15)
 //
 // Every product, sum and quotient is rounded on its own (no fused multiply-add): keys are rounded to fp16 and values next to
 // a rounding boundary take the code that the formula in fp32 gives, whoever evaluates it.
@@ -103,7 +103,7 @@ template <int D> __device__ __forceinline__ uint32_t quantise_row(const Eight &x
     mx = fmaxf(mx, lane_perm<0x141>(mx)), mn = fminf(mn, lane_perm<0x141>(mn));
     if constexpr (D == 128) mx = fmaxf(mx, lane_perm<0x140>(mx)), mn = fminf(mn, lane_perm<0x140>(mn));
     const float hi = clip * mx, lo = clip * mn;
-    scale = hi == lo ? 1.f : (hi - lo) / 15.f;
+    scale = hi == lo ? 1.f : (hi - lo) * (1.f / 15.f);
     zero = -rintf(lo / scale);
     uint32_t word = 0;
 #pragma unroll
