@@ -2,9 +2,9 @@
 //
 //   s_t = scale q . k_t,   o = sum_t softmax(s)_t v_t     over the tokens t < length whose page exists
 //
-// Bound by the bytes of the cache.  A workgroup takes one sequence, one key/value head (up to 16 of the query heads that share
-// it) and one run of tokens; its four waves walk over tiles of 32 tokens with a running maximum and sum, and meet in LDS.
-// Both products run on 16 x 16 x 32 matrix instructions with the query head in the columns:
+// Bound by the bytes of the cache.  A workgroup takes one key/value head (up to 16 of the query heads that share it) and runs of
+// tokens; its four waves walk over tiles of 32 tokens with a running maximum and sum, and meet in LDS.  Both products run on
+// 16 x 16 x 32 matrix instructions with the query head in the columns:
 //
 //   S^T = K Q^T   rows = tokens: lane (n, g) = (lane % 16, lane / 16) holds token n of the operand and gets tokens 4 g + r
 //   O^T = V^T P^T its k-index is the token: lane (n, g) supplies the eight tokens 4 g + r of two halves of the tile, which are
@@ -16,21 +16,21 @@
 // as exact as over c itself, to 2^-22, while over c 2^-24, bits 0-3, they are off by 2^-14 of a code.)  With scale d and zero z
 // per token,
 //   s_t = d (q . c - z sum(q)),   o = sum_t w_t (c_t - z_t),   w_t = p_t d_t
-// where d goes into the exponent, w = exp2(s log2(e) + log2(d) - maximum): weights then are at most 1 however large or small
-// the values are, and lose nothing to the range of fp16.  w is rounded to fp16 for the matrix pipe (half a step, 2^-12, per
-// token; the same rounded w multiplies z), sums and maxima are fp32.
-#include "sr_common.h"
+// where the maximum that is kept is that of s log2(e) + log2(d): weights w then are at most 2^8 however large or small the
+// values are, and lose nothing to the range of fp16.  w is rounded to fp16 for the matrix pipe (half a step, 2^-11 of it; the
+// same rounded w multiplies z), sums and maxima are fp32.
+#include "gemm_common.h"
 
 namespace sr {
 namespace {
 
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 union Frag { f16x8 v; uint32_t w[4]; _Float16 h[8]; };
 
-constexpr int kWaves = 4, kTile = 32;
+constexpr int kWaves = 4, kTile = 32, kRound = kWaves * kTile;
+constexpr int kLeast = 2;                                // rounds of a share, at least
 constexpr float kNone = -__builtin_inff();
 
 struct Decode {
@@ -47,13 +47,67 @@ struct Decode {
     int64_t max_len;                     // tokens that the page table covers
     const int32_t *lens;
     float scale;                         // times log2(e)
-    int splits, chunk;                   // runs of chunk tokens, a multiple of kWaves * kTile
+    int n_seqs, per_seq;                 // per_seq: key/value heads * row tiles
+    int shares;                          // workgroups that share the sequences of one of those; 0: one workgroup per sequence
     _Float16 *o;
     int64_t ldo;
-    float *part;                         // [sequence][head][split][D] sums, then [sequence][head][split][2] maximum, total
+    float *part;                         // [per_seq][share][2][row][D] sums, then [..][row][2] maximum, total
     float *part_ml;
 };
 
+// ---- the shares ------------------------------------------------------------------------------------------------------
+// The sequences' rounds (of kRound tokens, a tile per wave) lie behind each other in one line, and share w takes the rounds
+// [w, w + 1) * size of it: pieces of several sequences, or a piece of one.  Sizes follow from the lengths, which are known on
+// the device only, so every wave adds them up itself.  A sequence inside one share is finished there; else the share in which
+// it begins leaves a partial result in place 1, the others leave theirs in place 0, and the second kernel joins them.
+// (64 sequences of 0 .. 8192 tokens, 8 key/value heads of 128, 4 bits, 294 MB: the shares take 56 us, and cutting every sequence
+// into 2, 4 or 8 runs 74 - 77.)
+__device__ __forceinline__ int length_of(const Decode &a, int b) { return (int)min((int64_t)max(a.lens[b], 0), a.max_len); }
+__device__ __forceinline__ int rounds_of(const Decode &a, int b) { return b < a.n_seqs ? (length_of(a, b) + kRound - 1) / kRound : 0; }
+
+// sum over the lanes up to this one
+__device__ __forceinline__ int scan_of_wave(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);           // row_shr 1, 2, 4, 8 inside rows of 16,
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);          // the last lane of a row to the next row,
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);    // that of the first half to the second
+}
+// rounds in a share
+__device__ __forceinline__ int share_size(const Decode &a, int lane)
+{
+    int sum = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) sum += rounds_of(a, b0 + lane);
+    const int all = __builtin_amdgcn_readlane(scan_of_wave(sum), 63);
+    return max((all + a.shares - 1) / a.shares, kLeast);
+}
+// rounds of the sequences before b
+__device__ __forceinline__ int rounds_before(const Decode &a, int b, int lane)
+{
+    int sum = 0;
+    for (int b0 = 0; b0 < b; b0 += 64) sum += b0 + lane < b ? rounds_of(a, b0 + lane) : 0;
+    return __builtin_amdgcn_readlane(scan_of_wave(sum), 63);
+}
+// the sequence that holds round `at` of the line, and the rounds before it; n_seqs behind the last
+__device__ __forceinline__ int sequence_at(const Decode &a, int at, int lane, int &before)
+{
+    before = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+        const int n = rounds_of(a, b0 + lane), upto = before + scan_of_wave(n);
+        const unsigned long long past = __ballot(upto > at);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            before = __builtin_amdgcn_readlane(upto - n, l);
+            return b0 + l;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return a.n_seqs;
+}
+
+// ---- tiles -----------------------------------------------------------------------------------------------------------
 // reduction over the four lanes that share lane % 16
 __device__ __forceinline__ float max_of_groups(float v)
 {
@@ -75,109 +129,68 @@ __device__ __forceinline__ uint32_t nibble_pair(uint32_t w, int i)
     return (i == 0 ? w << 4 : w >> (4 * i - 4)) & 0x00F000F0u;
 }
 
-// what a wave loads of 32 tokens, as it lies in memory
+// A wave's share of 32 tokens in registers.  Whole runs of 16 tokens lie in one page, so that a half of the tile has one address
+// for the wave and fixed offsets per lane.
 template <int D, bool I4> struct Tile {
     static constexpr int KW = I4 ? D / 32 : D / 8;       // dwords of a lane's share of a key
     static constexpr int VW = I4 ? 1 : D / 32;           // dwords of a lane's share of a value
+    static constexpr int ROW = I4 ? D / 2 : D * 2;       // bytes of a row
     uint32_t k[2][KW], v[2][4][VW];
-    f32x4 kp[2][2], vp[2][2];                            // (scale, zero) of tokens 4 g + r
+    float ks[2][4], kz[2][4], vs[2][4], vz[2][4];        // scales and zeros of tokens 4 g + r of half u
 };
 
-template <int D, bool I4> __global__ __launch_bounds__(256) void attn_decode_kernel(Decode a)
-{
-    constexpr int C = D / 16;                            // output columns per lane and row index: d = C n + j
-    using T = Tile<D, I4>;
-    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t pairs = a.kv * a.row_tiles;
-    const uint32_t split = blockIdx.x % (uint32_t)a.splits, rest = blockIdx.x / (uint32_t)a.splits;
-    const uint32_t b = rest / pairs, pair = rest - b * pairs;
-    const uint32_t h = pair / a.row_tiles, row0 = 16 * (pair - h * a.row_tiles);
-    const int64_t len64 = min((int64_t)max(a.lens[b], 0), a.max_len);
-    const int len = (int)len64;
-    const int first = (int)split * a.chunk, last = min(first + a.chunk, len);
-    if (first >= len && a.splits > 1) return;            // the join goes by the length too
-    const int rows = min(16, a.group - (int)row0);
-    const int head0 = (int)(h * a.group + row0);
+// 4 bits: a tile waits in LDS as keys, values and parameters (two halves each; keys' first), two tiles per wave
+template <int D> struct Stage {
+    static constexpr int V = 16 * D, P = 32 * D, BYTES = 32 * D + 512;       // offsets of values and parameters
+};
 
-    // query row n of the tile in the order that the keys lie in
+// 16 bytes per lane from addresses of its own to LDS bytes [lds, lds + 1024), in the order of the lanes.  The cache is read once:
+// with loads that allocate in the caches 64 sequences of 4096 tokens (302 MB) took 77 us, with these 64.
+__device__ __forceinline__ void dma16_once(const void *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(p) : "memory", "m0");
+}
+
+// The query rows of a workgroup, and their state over the tokens that a wave has seen.
+template <int D, bool I4> struct Rows {
+    static constexpr int C = D / 16;                     // output columns per lane and row index: d = C n + j
+    using T = Tile<D, I4>;
     Frag q[D / 32];
-    float qsum = 0.f;
+    float unit, qz;                                      // score of one product; its sum(q)
+    f32x4 acc[C];                                        // sums of w c 2^-20, or w v
+    float top, total, zsum;                              // maximum; sums of p and w z over this lane's tokens
+
+    // row n of q, in the order that the keys lie in; zeros for a row that is not there
+    __device__ __forceinline__ void begin(const _Float16 *src, bool there, int g, float scale)
     {
-        const _Float16 *src = a.q + (int64_t)b * a.ldq + (int64_t)(head0 + n) * D;
-        const bool there = n < rows;
+        float qsum = 0.f;
         if constexpr (I4) {
             constexpr int per = D / 4;                   // codes of a key in one lane, a fragment per dword
-            _Float16 x[per];
 #pragma unroll
-            for (int i = 0; i < per; i += 8) {
+            for (int p = 0; p < per / 8; ++p) {
                 Frag f;
-                f.v = there ? *reinterpret_cast<const f16x8 *>(src + per * g + i) : (f16x8)(_Float16)0;
+                f.v = there ? *reinterpret_cast<const f16x8 *>(src + per * g + 8 * p) : (f16x8)(_Float16)0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[i + e] = f.h[e];
+                    q[p].h[e] = f.h[e / 2 + 4 * (e & 1)];                    // halves of nibble_pair()
                     qsum += (float)f.h[e];
                 }
             }
-#pragma unroll
-            for (int p = 0; p < per / 8; ++p)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) q[p].h[e] = x[8 * p + e / 2 + 4 * (e & 1)];      // halves of nibble_pair()
             qsum = sum_of_groups(qsum);
         } else {
 #pragma unroll
             for (int i = 0; i < D / 32; ++i) q[i].v = there ? *reinterpret_cast<const f16x8 *>(src + 32 * i + 8 * g) : (f16x8)(_Float16)0;
         }
+        unit = I4 ? scale * 1048576.f : scale, qz = qsum * scale;
+#pragma unroll
+        for (int j = 0; j < C; ++j) acc[j] = 0.f;
+        top = kNone, total = 0.f, zsum = 0.f;
     }
-    const float score_unit = I4 ? a.scale * 1048576.f : a.scale, qz = qsum * a.scale;
 
-    f32x4 acc[C];
-#pragma unroll
-    for (int j = 0; j < C; ++j) acc[j] = 0.f;
-    float top = kNone, total = 0.f, zsum = 0.f;          // total, zsum: over this lane's tokens
-
-    const int32_t *table = a.table + (int64_t)b * a.ld_table;
-    const int page_mask = (1 << a.page_shift) - 1;
-
-    for (int t0 = first + wave * kTile; t0 < last; t0 += kWaves * kTile) {
-        T t;
-        bool page_there[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            // 16 tokens lie in one page; tokens past the end read the last page there is and count for nothing
-            const int tu = min(t0 + 16 * u, (last - 1) & ~15);
-            const uint32_t id = (uint32_t)__builtin_amdgcn_readfirstlane(table[tu >> a.page_shift]);
-            page_there[u] = id < a.n_pages;
-            const int64_t row = ((((int64_t)(page_there[u] ? id : 0u) * a.kv + h) << a.page_shift) + (tu & page_mask));
-            if constexpr (I4) {
-                const uint32_t *kr = static_cast<const uint32_t *>(a.K) + (row + n) * (D / 8) + g * (D / 32);
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) t.k[u][i] = kr[i];
-                const uint32_t *vr = static_cast<const uint32_t *>(a.V) + (row + 4 * g) * (D / 8) + (D == 128 ? n : n >> 1);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) t.v[u][r][0] = vr[r * (D / 8)];
-                const f32x4 *kp = reinterpret_cast<const f32x4 *>(a.Kp + (row + 4 * g) * 2), *vp = reinterpret_cast<const f32x4 *>(a.Vp + (row + 4 * g) * 2);
-                t.kp[u][0] = kp[0], t.kp[u][1] = kp[1];
-                t.vp[u][0] = vp[0], t.vp[u][1] = vp[1];
-            } else {
-                const u32x4 *kr = reinterpret_cast<const u32x4 *>(static_cast<const _Float16 *>(a.K) + (row + n) * D);
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const u32x4 x = kr[4 * i + g];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) t.k[u][4 * i + e] = x[e];
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t *vr = reinterpret_cast<const uint32_t *>(static_cast<const _Float16 *>(a.V) + (row + 4 * g + r) * D) + n * (D / 32);
-#pragma unroll
-                    for (int e = 0; e < D / 32; ++e) t.v[u][r][e] = vr[e];
-                }
-            }
-        }
-
-        float s[2][4], vscale[2][4], vzero[2][4];
-        float most = kNone;
+    // 32 tokens from `at` on, those before `last` whose page is there (bit u: of half u)
+    __device__ __forceinline__ void use(T &t, int at, int last, uint32_t pages_there, int n, int g)
+    {
+        float y[2][4];                                   // scores over log(2); for 4 bits still without the key's scale
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f32x4 dot = 0.f;
@@ -189,56 +202,78 @@ template <int D, bool I4> __global__ __launch_bounds__(256) void attn_decode_ker
                 dot = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.v, q[i].v, dot, 0, 0, 0);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const bool there = page_there[u] && t0 + 16 * u + 4 * g + r < last;
-                if constexpr (I4) {
-                    const float ks = t.kp[u][r / 2][2 * (r % 2)], kz = t.kp[u][r / 2][2 * (r % 2) + 1];
-                    vscale[u][r] = there ? t.vp[u][r / 2][2 * (r % 2)] : 1.f;
-                    vzero[u][r] = there ? t.vp[u][r / 2][2 * (r % 2) + 1] : 0.f;
-                    const float x = ks * fmaf(dot[r], score_unit, -kz * qz) + __builtin_amdgcn_logf(vscale[u][r]);
-                    s[u][r] = there ? x : kNone;
-                } else {
-                    s[u][r] = there ? dot[r] * score_unit : kNone;
-#pragma unroll
-                    for (int e = 0; e < D / 32; ++e) t.v[u][r][e] = there ? t.v[u][r][e] : 0u;   // 0 times what lies there
-                }
-                most = fmaxf(most, s[u][r]);
-            }
+            for (int r = 0; r < 4; ++r) y[u][r] = I4 ? fmaf(dot[r], unit, -t.kz[u][r] * qz) : dot[r] * unit;
         }
-        most = fmaxf(top, max_of_groups(most));
-        const float base = most == kNone ? 0.f : most;
-        const float shrink = __builtin_amdgcn_exp2f(top - base);
-        total *= shrink;
-        zsum *= shrink;
-        top = most;
-        Frag w;
+        if (pages_there != 3 || at + kTile > last) {     // a token that is not there: score minus infinity, a finite value
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool there = (pages_there >> u & 1) && at + 16 * u + 4 * g + r < last;
+                    y[u][r] = there ? y[u][r] : kNone;
+                    if constexpr (I4) {
+                        t.ks[u][r] = there ? t.ks[u][r] : 1.f;
+                        t.vs[u][r] = there ? t.vs[u][r] : 1.f;
+                        t.vz[u][r] = there ? t.vz[u][r] : 0.f;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < T::VW; ++e) t.v[u][r][e] = there ? t.v[u][r][e] : 0u;
+                    }
+                }
+        }
+        float p[2][4], w[2][4];
+        auto weights = [&] {
+            float most = 0.f;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    p[u][r] = __builtin_amdgcn_exp2f(I4 ? fmaf(t.ks[u][r], y[u][r], -top) : y[u][r] - top);
+                    w[u][r] = I4 ? p[u][r] * t.vs[u][r] : p[u][r];
+                    most = fmaxf(most, w[u][r]);
+                }
+            return most;
+        };
+        // Weights stay below 2^8 relative to a maximum that is replaced only when one does not (the first tile's always): fp16
+        // has room for that, and most tiles then rescale nothing.
+        if (!__all(weights() <= 256.f && top != kNone)) {
+            float most = kNone;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    most = fmaxf(most, I4 ? fmaf(t.ks[u][r], y[u][r], __builtin_amdgcn_logf(t.vs[u][r])) : y[u][r]);
+            most = fmaxf(top, max_of_groups(most));
+            const float shrink = most == kNone ? 1.f : __builtin_amdgcn_exp2f(top - most);
+            total *= shrink;
+            zsum *= shrink;
+#pragma unroll
+            for (int j = 0; j < C; ++j) acc[j] *= shrink;
+            top = most == kNone ? 0.f : most;            // minus infinity from itself would be no number
+            weights();
+            top = most;
+        }
+        Frag f16w;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float p = __builtin_amdgcn_exp2f(s[u][r] - base);
-                w.h[4 * u + r] = (_Float16)p;
-                if constexpr (I4) {
-                    total = fmaf(p, __builtin_amdgcn_rcpf(vscale[u][r]), total);
-                    zsum = fmaf((float)w.h[4 * u + r], vzero[u][r], zsum);
-                } else {
-                    total += p;
-                }
+                f16w.h[4 * u + r] = (_Float16)w[u][r];
+                total += p[u][r];
+                if constexpr (I4) zsum = fmaf((float)f16w.h[4 * u + r], t.vz[u][r], zsum);
             }
-#pragma unroll
-        for (int j = 0; j < C; ++j) acc[j] *= shrink;
-        // half j of the row of token pairs (r, r + 1): two tokens per dword
+        // column j of token pairs (r, r + 1): two tokens per dword
         uint32_t lo[2][2], hi[2][2];
         if constexpr (I4) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const uint32_t x = t.v[u][2 * p][0], y = t.v[u][2 * p + 1][0];
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t x = t.v[u][2 * i][0], z = t.v[u][2 * i + 1][0];
                     if constexpr (D == 128) {
-                        lo[u][p] = low_halves(x, y), hi[u][p] = high_halves(x, y);
+                        lo[u][i] = low_halves(x, z), hi[u][i] = high_halves(x, z);
                     } else {
-                        lo[u][p] = __builtin_amdgcn_perm(y, x, n & 1 ? 0x07060302u : 0x05040100u), hi[u][p] = 0;
+                        lo[u][i] = __builtin_amdgcn_perm(z, x, n & 1 ? 0x07060302u : 0x05040100u), hi[u][i] = 0;
                     }
                 }
         }
@@ -248,126 +283,357 @@ template <int D, bool I4> __global__ __launch_bounds__(256) void attn_decode_ker
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
+                for (int i = 0; i < 2; ++i) {
                     if constexpr (I4) {
-                        const uint32_t x = j < 4 ? lo[u][p] : hi[u][p];
-                        f.w[2 * u + p] = nibble_pair(x, j & 3);
+                        f.w[2 * u + i] = nibble_pair(j < 4 ? lo[u][i] : hi[u][i], j & 3);
                     } else {
-                        const uint32_t x = t.v[u][2 * p][j / 2], y = t.v[u][2 * p + 1][j / 2];
-                        f.w[2 * u + p] = j & 1 ? high_halves(x, y) : low_halves(x, y);
+                        const uint32_t x = t.v[u][2 * i][j / 2], z = t.v[u][2 * i + 1][j / 2];
+                        f.w[2 * u + i] = j & 1 ? high_halves(x, z) : low_halves(x, z);
                     }
                 }
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.v, w.v, acc[j], 0, 0, 0);
+            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.v, f16w.v, acc[j], 0, 0, 0);
         }
     }
+};
 
-    // the four waves meet: acc[j][r] of lane (n, g) is column d = C (4 g + r) + j of query row n
-    __shared__ float s_top[kWaves][16], s_total[kWaves][16];
-    __shared__ float s_acc[kWaves][16][D + 4];
-    total = sum_of_groups(total);
-    zsum = sum_of_groups(zsum);
-    if (g == 0) s_top[wave][n] = top, s_total[wave][n] = total;
+// Tokens [first, last) of sequence b over a wave's tiles, `smem` the wave's own stages (4 bits).
+template <int D, bool I4>
+__device__ __forceinline__ void walk(const Decode &a, Rows<D, I4> &rows, int b, int h, int first, int last, uint8_t *smem, int wave, int lane)
+{
+    using T = Tile<D, I4>;
+    const int n = lane & 15, g = lane >> 4;
+    // (constant while the kernel runs: scalar loads, which the vector counter does not see)
+    const auto *table = (const __attribute__((address_space(4))) int32_t *)(uintptr_t)(a.table + (int64_t)b * a.ld_table);
+    const int page_mask = (1 << a.page_shift) - 1;
+    // Tokens past the end read the last rows there are and count for nothing; so do those of a page that does not exist, from
+    // page 0.  `there`: bit u, the page of half u exists.
+    struct Where { int64_t row0, row1; uint32_t there; };
+    struct Pages { int id[2]; };
+    auto half_at = [&](int t0, int u) { return min(t0 + 16 * u, (last - 1) & ~15); };
+    auto pages_of = [&](int t0) {
+        Pages p;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+        for (int u = 0; u < 2; ++u) p.id[u] = table[half_at(t0, u) >> a.page_shift];
+        return p;
+    };
+    auto where = [&](int t0, const Pages &p) {
+        Where w;
+        w.there = 0;
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            float x = acc[j][r];
-            if constexpr (I4) x = x * 1048576.f - zsum;
-            s_acc[wave][n][C * (4 * g + r) + j] = x;
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t id = (uint32_t)__builtin_amdgcn_readfirstlane(p.id[u]);
+            const bool there = id < a.n_pages;
+            w.there |= there ? 1u << u : 0u;
+            (u ? w.row1 : w.row0) = (((int64_t)(there ? id : 0u) * a.kv + h) << a.page_shift) + (half_at(t0, u) & page_mask);
         }
-    __syncthreads();
-    for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
-        const int m = i / (D / 4), d = 4 * (i % (D / 4));
-        float most = s_top[0][m];
+        return w;
+    };
+    auto half_of = [&](const void *side, int64_t row) { return static_cast<const uint8_t *>(side) + row * T::ROW; };
+
+    int t0 = first + wave * kTile;
+    if (t0 >= last) return;
+    if constexpr (I4) {
+        // Rows come by DMA into two stages of the wave's own, a tile being loaded while another waits: registers hold one tile.
+        // Page numbers are fetched a tile before that.  Lanes load in the order of memory; keys land with the chunks of row n
+        // swapped by n / 4 and values with the rows in the order 4 (t % 4) + t / 4, so that both are read back without bank
+        // conflicts.  A stage is loaded again behind a wait for the reads of it.
+        constexpr int CPR = D / 32;                      // 16-byte chunks of a row
+        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
+        const int row = (lane / CPR) & 15, chunk = lane % CPR;
+        const uint32_t k_off = row * T::ROW + 16 * (D == 128 ? chunk ^ (row >> 2) : chunk);
+        const uint32_t v_off = (D == 128 ? 4 * (row & 3) + (row >> 2) : row) * T::ROW + 16 * chunk;
+        auto load = [&](int slot, const Where &w) {
+            const uint32_t to = lds + slot * Stage<D>::BYTES;
+            if constexpr (D == 128) {
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) most = fmaxf(most, s_top[w][m]);
-        const float base = most == kNone ? 0.f : most;
-        f32x4 sum = 0.f;
-        float all = 0.f;
+                for (int u = 0; u < 2; ++u) {
+                    dma16_once(half_of(a.K, u ? w.row1 : w.row0) + k_off, to + 1024 * u);
+                    dma16_once(half_of(a.V, u ? w.row1 : w.row0) + v_off, to + Stage<D>::V + 1024 * u);
+                }
+            } else {                                     // both halves at once
+                dma16_once(half_of(a.K, w.row0 + (lane < 32 ? 0 : w.row1 - w.row0)) + k_off, to);
+                dma16_once(half_of(a.V, w.row0 + (lane < 32 ? 0 : w.row1 - w.row0)) + v_off, to + Stage<D>::V);
+            }
+            if (lane < 32)                               // keys' two halves, then values'
+                dma16_once(reinterpret_cast<const uint8_t *>(lane < 16 ? a.Kp : a.Vp) + (w.row0 + (lane & 8 ? w.row1 - w.row0 : 0)) * 8 + 16 * (lane & 7), to + Stage<D>::P);
+        };
+        constexpr int LOADS = D == 128 ? 5 : 3;          // of a tile
+        auto fetch = [&](T &t, int slot) {
+            const uint8_t *from = smem + slot * Stage<D>::BYTES;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float e = __builtin_amdgcn_exp2f(s_top[w][m] - base);
-            sum += e * *reinterpret_cast<const f32x4 *>(&s_acc[w][m][d]);
-            all += e * s_total[w][m];
+            for (int u = 0; u < 2; ++u) {
+                if constexpr (D == 128) {
+                    const u32x4 x = *reinterpret_cast<const u32x4 *>(from + 1024 * u + 64 * n + 16 * (g ^ (n >> 2)));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t.k[u][i] = x[i];
+                } else {
+                    const u32x2 x = *reinterpret_cast<const u32x2 *>(from + 512 * u + 32 * n + 8 * g);
+                    t.k[u][0] = x[0], t.k[u][1] = x[1];
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    t.v[u][r][0] = *reinterpret_cast<const uint32_t *>(from + Stage<D>::V + (D == 128 ? 1024 * u + 64 * (4 * r + g) + 4 * n : 512 * u + 32 * (4 * g + r) + 4 * (n >> 1)));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const f32x4 kp = *reinterpret_cast<const f32x4 *>(from + Stage<D>::P + 128 * u + 32 * g + 16 * i);
+                    const f32x4 vp = *reinterpret_cast<const f32x4 *>(from + Stage<D>::P + 256 + 128 * u + 32 * g + 16 * i);
+                    t.ks[u][2 * i] = kp[0], t.kz[u][2 * i] = kp[1], t.ks[u][2 * i + 1] = kp[2], t.kz[u][2 * i + 1] = kp[3];
+                    t.vs[u][2 * i] = vp[0], t.vz[u][2 * i] = vp[1], t.vs[u][2 * i + 1] = vp[2], t.vz[u][2 * i + 1] = vp[3];
+                }
+            }
+        };
+        Where w = where(t0, pages_of(t0));
+        uint32_t there = w.there, there_next = 0;
+        load(0, w);
+        if (t0 + kRound < last) {
+            w = where(t0 + kRound, pages_of(t0 + kRound));
+            there_next = w.there;
+            load(1, w);
         }
-        if (a.splits == 1) {
-            const float norm = all > 0.f ? 1.f / all : 0.f;
-            _Float16 y[4];
+        Pages next = pages_of(t0 + 2 * kRound);
+        for (int slot = 0; t0 < last; t0 += kRound, slot ^= 1) {
+            T t;
+            if (t0 + kRound < last) wait_vmcnt<LOADS>();
+            else wait_vmcnt<0>();
+            fetch(t, slot);
+            const uint32_t here = there;
+            there = there_next;
+            if (t0 + 2 * kRound < last) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                w = where(t0 + 2 * kRound, next);
+                there_next = w.there;
+                load(slot, w);
+                next = pages_of(t0 + 3 * kRound);
+            }
+            rows.use(t, t0, last, here, n, g);
+        }
+    } else {
+        for (; t0 < last; t0 += kRound) {
+            T t;
+            const Where w = where(t0, pages_of(t0));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (_Float16)(sum[e] * norm);
-            *reinterpret_cast<u32x2 *>(a.o + (int64_t)b * a.ldo + (int64_t)(head0 + m) * D + d) = *reinterpret_cast<u32x2 *>(y);
-        } else {
-            const int64_t at = ((int64_t)b * a.heads + head0 + m) * a.splits + split;
-            *reinterpret_cast<f32x4 *>(a.part + at * D + d) = sum;
-            if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(most, all);
+            for (int u = 0; u < 2; ++u) {
+                const uint8_t *kb = half_of(a.K, u ? w.row1 : w.row0), *vb = half_of(a.V, u ? w.row1 : w.row0);
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) {
+                    const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kb + (uint32_t)(n * T::ROW + 16 * g + 64 * i)));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t.k[u][4 * i + e] = x[e];
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint8_t *p = vb + (uint32_t)((4 * g + r) * T::ROW + n * (D / 8));
+                    if constexpr (D == 128) {
+                        const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) t.v[u][r][e] = x[e];
+                    } else {
+                        const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p));
+                        t.v[u][r][0] = x[0], t.v[u][r][1] = x[1];
+                    }
+                }
+            }
+            rows.use(t, t0, last, w.there, n, g);
         }
     }
 }
 
-// the runs of one query head, joined by one workgroup: D / 4 threads per part of the runs
-template <int D> __global__ __launch_bounds__(256) void attn_join_kernel(Decode a)
+template <int D> __device__ __forceinline__ void store_row(_Float16 *dst, f32x4 sum, float total)
 {
-    constexpr int TPR = D / 4, PARTS = 256 / TPR;
-    const uint32_t row = blockIdx.x;                     // sequence * heads + head
-    const uint32_t b = row / a.heads, head = row - b * a.heads;
-    const int64_t len = min((int64_t)max(a.lens[b], 0), a.max_len);
-    const int runs = (int)((len + a.chunk - 1) / a.chunk);
-    const int part = threadIdx.x / TPR, d = 4 * (threadIdx.x % TPR);
-    const float *ml = a.part_ml + (int64_t)row * a.splits * 2, *sums = a.part + (int64_t)row * a.splits * D;
+    const float norm = total > 0.f ? 1.f / total : 0.f;
+    union { _Float16 h[4]; u32x2 v; } y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y.h[e] = (_Float16)(sum[e] * norm);
+    *reinterpret_cast<u32x2 *>(dst) = y.v;
+}
+
+template <int D, bool I4> __global__ __launch_bounds__(kWaves * 64, 2) void attn_decode_kernel(Decode a)
+{
+    constexpr int C = D / 16;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Neighbouring workgroups take different heads, so that an XCD, every eighth workgroup of a launch, gets as much as any.
+    const int block = (int)(blockIdx.x / (uint32_t)a.per_seq), pair = (int)blockIdx.x - block * a.per_seq;
+    const int h = pair / a.row_tiles, row0 = 16 * (pair - h * a.row_tiles);
+    const int n_rows = min(16, a.group - row0), head0 = h * a.group + row0;
+    int b = block, before = 0, from = 0, to = 0;         // sequence, rounds before it; the rounds of this share
+    if (a.shares) {
+        const int size = share_size(a, lane);
+        from = block * size, to = from + size;
+        b = sequence_at(a, from, lane, before);
+        if (b == a.n_seqs) return;
+    }
+    for (;;) {
+        const int len = length_of(a, b), rounds = (len + kRound - 1) / kRound;
+        const int r0 = max(from - before, 0), r1 = a.shares ? min(to - before, rounds) : rounds;
+        const bool whole = r0 == 0 && r1 == rounds;
+        Rows<D, I4> rows;
+        rows.begin(a.q + (int64_t)b * a.ldq + (int64_t)(head0 + n) * D, n < n_rows, g, a.scale);
+        walk<D, I4>(a, rows, b, h, r0 * kRound, min(r1 * kRound, len), smem + wave * (2 * Stage<D>::BYTES), wave, lane);
+        __syncthreads();                                 // the stages' area is used again
+
+        // the four waves meet: acc[j][r] of lane (n, g) is column d = C (4 g + r) + j of query row n
+        float(*s_top)[16] = reinterpret_cast<float(*)[16]>(smem), (*s_total)[16] = s_top + kWaves;
+        float(*s_acc)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(s_total + kWaves);
+        const float total = sum_of_groups(rows.total), zsum = sum_of_groups(rows.zsum);
+        if (g == 0) s_top[wave][n] = rows.top, s_total[wave][n] = total;
+        if (n < n_rows) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int j = 0; j < C; j += 4) {
+                    f32x4 x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = I4 ? rows.acc[j + e][r] * 1048576.f - zsum : rows.acc[j + e][r];
+                    *reinterpret_cast<f32x4 *>(&s_acc[wave][n][C * (4 * g + r) + j]) = x;
+                }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < n_rows * (D / 4); i += kWaves * 64) {
+            const int m = i / (D / 4), d = 4 * (i % (D / 4));
+            float most = s_top[0][m];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) most = fmaxf(most, s_top[w][m]);
+            const float base = most == kNone ? 0.f : most;
+            f32x4 sum = 0.f;
+            float all = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float e = __builtin_amdgcn_exp2f(s_top[w][m] - base);
+                sum += e * *reinterpret_cast<const f32x4 *>(&s_acc[w][m][d]);
+                all += e * s_total[w][m];
+            }
+            if (whole) {
+                store_row<D>(a.o + (int64_t)b * a.ldo + (int64_t)(head0 + m) * D + d, sum, all);
+            } else {
+                const int64_t at = (((int64_t)pair * a.shares + block) * 2 + (r0 == 0)) * min(16, a.group) + m;
+                *reinterpret_cast<f32x4 *>(a.part + at * D + d) = sum;
+                if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(most, all);
+            }
+        }
+        if (!a.shares) return;
+        // on to the next sequence of the share that has tokens
+        do before += rounds_of(a, b++);
+        while (b < a.n_seqs && before < to && rounds_of(a, b) == 0);
+        if (b >= a.n_seqs || before >= to) return;
+        __syncthreads();
+    }
+}
+
+// The pieces of query heads joined: D / 4 lanes take four columns each of every PARTS-th piece of a head, four pieces in flight;
+// the parts of a head meet in LDS.  Sequences without tokens get their zeros here too.
+template <int D, int PARTS> __global__ __launch_bounds__(256) void attn_join_kernel(Decode a, uint32_t n_rows)
+{
+    constexpr int TPR = D / 4, ROWS = 256 / (TPR * PARTS), DEEP = 4;
+    const int lane = threadIdx.x % TPR, part = threadIdx.x / TPR % PARTS, mine = threadIdx.x / (TPR * PARTS), d = 4 * lane;
+    const uint32_t row = min(blockIdx.x * ROWS + mine, n_rows - 1);          // sequence * heads + head
+    const int b = (int)(row / a.heads), head = (int)(row - (uint32_t)b * a.heads);
+    int pieces = 0, first = 0;                                               // of this row's sequence; the first one's share
+    {
+        // the rows of a workgroup may belong to several sequences: one after the other, by every wave
+        const int size = share_size(a, threadIdx.x & 63);
+        const int b_low = (int)(min(blockIdx.x * ROWS, n_rows - 1) / a.heads), b_high = (int)(min(blockIdx.x * ROWS + ROWS - 1, n_rows - 1) / a.heads);
+        int before = rounds_before(a, b_low, threadIdx.x & 63);
+        for (int s = b_low; s <= b_high; ++s) {
+            const int rounds = rounds_of(a, s);
+            if (s == b) {
+                first = before / size;
+                pieces = rounds ? (before + rounds - 1) / size - first + 1 : 0;
+            }
+            before += rounds;
+        }
+    }
+    const int h = head / a.group, in_group = head - h * a.group, group_rows = min(16, a.group);
+    const int64_t place = ((int64_t)(h * a.row_tiles + in_group / 16) * a.shares + first) * 2;
+    auto at = [&](int i) { return (place + 2 * i + (i == 0)) * group_rows + in_group % 16; };
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
     float most = kNone, all = 0.f;
     f32x4 sum = 0.f;
-    for (int i = part; i < runs; i += PARTS) {
-        const float2 x = reinterpret_cast<const float2 *>(ml)[i];
-        const f32x4 y = *reinterpret_cast<const f32x4 *>(sums + (int64_t)i * D + d);
-        const float now = fmaxf(most, x.x), base = now == kNone ? 0.f : now;
-        const float shrink = __builtin_amdgcn_exp2f(most - base), e = __builtin_amdgcn_exp2f(x.x - base);
-        sum = sum * shrink + y * e;
-        all = all * shrink + x.y * e;
+    for (int i0 = pieces > 1 ? part : pieces; i0 < pieces; i0 += PARTS * DEEP) {   // (a sequence in one piece is done)
+        float2 x[DEEP];
+        f32x4 y[DEEP];
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            const int64_t p = at(min(i0 + PARTS * k, pieces - 1));
+            x[k] = ml[p];
+            y[k] = *reinterpret_cast<const f32x4 *>(a.part + p * D + d);
+        }
+        float now = most;
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            x[k].x = i0 + PARTS * k < pieces ? x[k].x : kNone;
+            now = fmaxf(now, x[k].x);
+        }
+        const float base = now == kNone ? 0.f : now, shrink = __builtin_amdgcn_exp2f(most - base);
+        sum *= shrink;
+        all *= shrink;
+#pragma unroll
+        for (int k = 0; k < DEEP; ++k) {
+            const float e = __builtin_amdgcn_exp2f(x[k].x - base);
+            sum += y[k] * e;
+            all += x[k].y * e;
+        }
         most = now;
     }
-    __shared__ float s_top[PARTS], s_total[PARTS];
-    __shared__ f32x4 s_sum[PARTS][TPR];
-    if (d == 0) s_top[part] = most, s_total[part] = all;
-    s_sum[part][d / 4] = sum;
-    __syncthreads();
-    if (part) return;
-    float top = s_top[0];
+    if constexpr (PARTS > 1) {
+        __shared__ float s_top[ROWS][PARTS], s_total[ROWS][PARTS];
+        __shared__ f32x4 s_sum[ROWS][PARTS][TPR];
+        if (lane == 0) s_top[mine][part] = most, s_total[mine][part] = all;
+        s_sum[mine][part][lane] = sum;
+        __syncthreads();
+        if (part) return;
 #pragma unroll
-    for (int p = 1; p < PARTS; ++p) top = fmaxf(top, s_top[p]);
-    const float base = top == kNone ? 0.f : top;
-    sum = 0.f, all = 0.f;
+        for (int p = 1; p < PARTS; ++p) most = fmaxf(most, s_top[mine][p]);
+        const float base = most == kNone ? 0.f : most;
+        sum = 0.f, all = 0.f;
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-        const float e = __builtin_amdgcn_exp2f(s_top[p] - base);
-        sum += s_sum[p][d / 4] * e;
-        all += s_total[p] * e;
+        for (int p = 0; p < PARTS; ++p) {
+            const float e = __builtin_amdgcn_exp2f(s_top[mine][p] - base);
+            sum += s_sum[mine][p][lane] * e;
+            all += s_total[mine][p] * e;
+        }
     }
-    const float norm = all > 0.f ? 1.f / all : 0.f;
-    _Float16 y[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (_Float16)(sum[e] * norm);
-    *reinterpret_cast<u32x2 *>(a.o + (int64_t)b * a.ldo + (int64_t)head * D + d) = *reinterpret_cast<u32x2 *>(y);
+    if (pieces == 1 || blockIdx.x * ROWS + mine >= n_rows) return;
+    store_row<D>(a.o + (int64_t)b * a.ldo + (int64_t)head * D + d, sum, all);
 }
 
-// Runs per sequence: enough workgroups for four on every compute unit, none shorter than one round of the waves.
-struct Runs { int splits, chunk; };
-Runs runs_of(int64_t n_seqs, int64_t kv, int64_t group, int64_t max_len)
+template <int D, bool I4> hipError_t launch_shares(const Decode &a, hipStream_t st)
 {
-    constexpr int64_t round = kWaves * kTile;
-    const int64_t pairs = n_seqs * kv * ((group + 15) / 16), want = (int64_t)compute_units() * 4;
-    const int64_t rounds = (max_len + round - 1) / round;
-    int64_t splits = (want + pairs - 1) / pairs;
-    if (splits > rounds) splits = rounds;
-    const int64_t chunk = (rounds + splits - 1) / splits * round;
-    return {(int)((max_len + chunk - 1) / chunk), (int)chunk};
+    constexpr int meet = kWaves * 16 * (D + 4 + 2) * 4, stages = I4 ? kWaves * 2 * Stage<D>::BYTES : 0;
+    constexpr int lds = meet > stages ? meet : stages;
+    static_assert(lds <= 65536, "within the default limit of dynamic LDS");
+    const dim3 grid((unsigned)(a.shares ? a.shares : a.n_seqs) * (unsigned)a.per_seq);
+    hipLaunchKernelGGL((attn_decode_kernel<D, I4>), grid, dim3(kWaves * 64), lds, st, a);
+    return hipGetLastError();
+}
+
+template <int D> hipError_t launch_join(const Decode &a, hipStream_t st)
+{
+    constexpr int groups = 256 / (D / 4);
+    const uint32_t n_rows = (uint32_t)a.n_seqs * (uint32_t)a.heads;
+    if (a.shares > 4 * a.n_seqs) hipLaunchKernelGGL((attn_join_kernel<D, groups>), dim3(n_rows), dim3(256), 0, st, a, n_rows);
+    else hipLaunchKernelGGL((attn_join_kernel<D, 1>), dim3((n_rows + groups - 1) / groups), dim3(256), 0, st, a, n_rows);
+    return hipGetLastError();
+}
+
+// Shares of the sequences of one key/value head and row tile; 0: a workgroup per sequence does it all, which needs no second
+// kernel.
+int shares_of(int64_t n_seqs, int64_t per_seq, int64_t max_len)
+{
+    const int64_t want = (int64_t)compute_units() * 2;
+    const int64_t shares = want / per_seq;
+    if (shares < 2 || n_seqs > 1024 || n_seqs * per_seq >= 4 * want || max_len <= kLeast * kRound) return 0;
+    if (n_seqs * ((max_len + kRound - 1) / kRound) >= 1 << 30) return 0;     // rounds are counted in 32 bits
+    return (int)shares;
 }
 
 }  // namespace
 
 size_t attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t kv, int64_t dim, int64_t max_len)
 {
-    const Runs r = runs_of(n_seqs, kv, n_heads / kv, max_len);
-    return r.splits > 1 ? (size_t)n_seqs * n_heads * r.splits * (dim + 2) * 4 : 0;
+    const int64_t group = n_heads / kv, per_seq = kv * ((group + 15) / 16);
+    return (size_t)(per_seq * shares_of(n_seqs, per_seq, max_len) * 2 * (group < 16 ? group : 16) * (dim + 2) * 4);
 }
 
 hipError_t launch_attn_decode(const void *Q, int64_t ldq, int64_t n_seqs, int64_t n_heads, const KvCache &c, const int32_t *table,
@@ -375,28 +641,20 @@ hipError_t launch_attn_decode(const void *Q, int64_t ldq, int64_t n_seqs, int64_
                               void *workspace, hipStream_t st)
 {
     Decode a;
-    const int64_t max_len = max_pages * c.page_size;
-    const Runs r = runs_of(n_seqs, c.heads, n_heads / c.heads, max_len);
     a.q = static_cast<const _Float16 *>(Q), a.ldq = ldq;
     a.heads = (int)n_heads, a.kv = (int)c.heads, a.group = (int)(n_heads / c.heads), a.row_tiles = (a.group + 15) / 16;
     a.K = c.K, a.V = c.V, a.Kp = c.Kp, a.Vp = c.Vp;
     a.n_pages = (uint32_t)c.pages, a.page_shift = __builtin_ctzll((unsigned long long)c.page_size);
-    a.table = table, a.ld_table = ld_table, a.max_len = max_len, a.lens = lens;
+    a.table = table, a.ld_table = ld_table, a.max_len = max_pages * c.page_size, a.lens = lens;
     a.scale = scale * 1.4426950408889634f;
-    a.splits = r.splits, a.chunk = r.chunk;
+    a.n_seqs = (int)n_seqs, a.per_seq = a.kv * a.row_tiles, a.shares = shares_of(n_seqs, a.per_seq, a.max_len);
     a.o = static_cast<_Float16 *>(O), a.ldo = ldo;
     a.part = static_cast<float *>(workspace);
-    a.part_ml = a.part + (size_t)n_seqs * n_heads * r.splits * c.dim;
-    const dim3 grid((unsigned)(n_seqs * c.heads * a.row_tiles * r.splits)), block(kWaves * 64);
-    if (c.dim == 128 && c.i4) hipLaunchKernelGGL((attn_decode_kernel<128, true>), grid, block, 0, st, a);
-    else if (c.dim == 128) hipLaunchKernelGGL((attn_decode_kernel<128, false>), grid, block, 0, st, a);
-    else if (c.i4) hipLaunchKernelGGL((attn_decode_kernel<64, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((attn_decode_kernel<64, false>), grid, block, 0, st, a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || r.splits == 1) return e;
-    const dim3 rows((unsigned)(n_seqs * n_heads));
-    if (c.dim == 128) hipLaunchKernelGGL((attn_join_kernel<128>), rows, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((attn_join_kernel<64>), rows, dim3(256), 0, st, a);
-    return hipGetLastError();
+    a.part_ml = a.part + (size_t)a.per_seq * a.shares * 2 * (a.group < 16 ? a.group : 16) * c.dim;
+    const hipError_t e = c.dim == 128 ? (c.i4 ? launch_shares<128, true>(a, st) : launch_shares<128, false>(a, st))
+                                      : (c.i4 ? launch_shares<64, true>(a, st) : launch_shares<64, false>(a, st));
+    if (e != hipSuccess || !a.shares) return e;
+    return c.dim == 128 ? launch_join<128>(a, st) : launch_join<64>(a, st);
 }
 
 }  // namespace sr
