@@ -33,7 +33,7 @@ struct Prefill {
     int n_seqs, tokens_q, tokens_k;
     int heads, kv, tiles;                                // tiles: of query rows, an upper bound
     int causal;
-    float scale;                                         // times log2(e)
+    float scale, per_scale;                              // times log2(e); its reciprocal
     _Float16 *o;
     int64_t ldo;
 };
@@ -73,7 +73,7 @@ __device__ __forceinline__ bool find_tile(const Prefill &a, int tile, int lane, 
     return false;
 }
 
-template <int D> __global__ __launch_bounds__(256) void attn_prefill_kernel(Prefill a)
+template <int D> __global__ __launch_bounds__(256, 2) void attn_prefill_kernel(Prefill a)
 {
     constexpr int CH = D / 8;                            // 16-byte chunks of a row
     constexpr uint32_t kTileBytes = kKeys * D * 2;
@@ -107,7 +107,9 @@ template <int D> __global__ __launch_bounds__(256) void attn_prefill_kernel(Pref
     f32x16 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = 0.f;
-    float top = kNone, total = 0.f;
+    // Weights are exp2(score - base), a row's largest about 2^7 when base is set, and base is set again only where one would pass
+    // 2^15: fp16 has room for that, its subnormals begin 2^-21 below the largest, and most tiles rescale nothing.
+    float top = kNone, limit = kNone, base = 0.f, total = 0.f;
 
     // Tiles lie in LDS by rows, their chunks swapped so that the lanes that read at once meet every bank: keys, read 32 rows
     // of one chunk at a time, by row; values, read 4 rows of four neighbouring chunks, by row in steps of four chunks.
@@ -115,82 +117,102 @@ template <int D> __global__ __launch_bounds__(256) void attn_prefill_kernel(Pref
     const uint8_t *vb = reinterpret_cast<const uint8_t *>(a.v + (int64_t)k0 * a.ldv + (int64_t)kvh * D);
     auto key_swap = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
     auto value_swap = [](int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; };
+    uint32_t k_off[LOADS], v_off[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int at = (i * 4 + wave) * 64 + lane, r = at / CH, c = at % CH;
+        k_off[i] = r * (uint32_t)(a.ldk * 2) + 16 * (c ^ key_swap(r));
+        v_off[i] = r * (uint32_t)(a.ldv * 2) + 16 * (c ^ value_swap(r));
+    }
     auto load = [&](int t0, int slot) {
         const uint8_t *kt = kb + (int64_t)t0 * a.ldk * 2, *vt = vb + (int64_t)t0 * a.ldv * 2;
+        const uint32_t to = lds + slot * 2 * kTileBytes + wave * 1024;
+        if (t0 + kKeys <= nk) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int piece = i * 4 + wave, at = piece * 64 + lane, r = at / CH, c = at % CH;
-            const uint32_t rr = (uint32_t)min(r, nk - 1 - t0);                         // rows past the end: the last one again
-            const uint32_t to = lds + slot * 2 * kTileBytes + piece * 1024;
-            dma16(kt, rr * (uint32_t)(a.ldk * 2) + 16 * (c ^ key_swap(r)), to);
-            dma16(vt, rr * (uint32_t)(a.ldv * 2) + 16 * (c ^ value_swap(r)), to + kTileBytes);
+            for (int i = 0; i < LOADS; ++i) {
+                dma16(kt, k_off[i], to + 4096 * i);
+                dma16(vt, v_off[i], to + 4096 * i + kTileBytes);
+            }
+        } else {                                         // rows past the end: the last one again
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int r = ((i * 4 + wave) * 64 + lane) / CH;
+                const uint32_t over = (uint32_t)max(r - (nk - 1 - t0), 0);
+                dma16(kt, k_off[i] - over * (uint32_t)(a.ldk * 2), to + 4096 * i);
+                dma16(vt, v_off[i] - over * (uint32_t)(a.ldv * 2), to + 4096 * i + kTileBytes);
+            }
         }
     };
 
-    const int n_tiles = end > 0 ? (end + kKeys - 1) / kKeys : 0;
-    if (n_tiles) load(0, 0);
-    for (int i = 0; i < n_tiles; ++i) {
-        const int t0 = i * kKeys;
+    const int n_tiles = end > 0 ? (end + kKeys - 1) / kKeys : 0, mine = wend > 0 ? (wend + kKeys - 1) / kKeys : 0;
+    // the tile that was asked for a round ago is there, and everybody is done with the slot of the next one
+    auto turn = [&](int i) {
         wait_vmcnt<0>();
         barrier_nofence();
-        if (i + 1 < n_tiles) load(t0 + kKeys, (i + 1) & 1);
-        if (t0 < wend) {
-            const uint8_t *ks = smem + (i & 1) * 2 * kTileBytes, *vs = ks + kTileBytes;
-            f32x16 s[2];
+        if (i + 1 < n_tiles) load((i + 1) * kKeys, (i + 1) & 1);
+    };
+    if (n_tiles) load(0, 0);
+    for (int i = 0; i < mine; ++i) {
+        const int t0 = i * kKeys;
+        turn(i);
+        const uint8_t *ks = smem + (i & 1) * 2 * kTileBytes, *vs = ks + kTileBytes;
+        f32x16 s[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                s[u] = 0.f;
-                const int r = 32 * u + m;
+        for (int u = 0; u < 2; ++u) {
+            s[u] = 0.f;
+            const int r = 32 * u + m;
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) {
-                    Frag k;
-                    k.v = *reinterpret_cast<const f16x8 *>(ks + r * (D * 2) + 16 * ((2 * d + g) ^ key_swap(r)));
-                    s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k.v, q[d].v, s[u], 0, 0, 0);
-                }
+            for (int d = 0; d < D / 16; ++d) {
+                Frag k;
+                k.v = *reinterpret_cast<const f16x8 *>(ks + r * (D * 2) + 16 * ((2 * d + g) ^ key_swap(r)));
+                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k.v, q[d].v, s[u], 0, 0, 0);
             }
-            if (t0 + kKeys > whole) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (t0 + 32 * u + 8 * (e / 4) + 4 * g + (e & 3) >= rend) s[u][e] = kNone;
-            }
-            float most = top;
+        }
+        if (t0 + kKeys > whole) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) most = fmaxf(most, s[u][e]);
-            most = fmaxf(most, __shfl_xor(most, 32, 64));
-            const float base = most == kNone ? 0.f : most * a.scale;
-            const float shrink = __builtin_amdgcn_exp2f(fmaf(top, a.scale, -base));
-            top = most;
+                for (int e = 0; e < 16; ++e)
+                    if (t0 + 32 * u + 8 * (e / 4) + 4 * g + (e & 3) >= rend) s[u][e] = kNone;
+        }
+        float most = kNone;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[u][e]);
+        if (!__all(most <= limit)) {
+            most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), top);
+            const float shrink = most == kNone ? 1.f : __builtin_amdgcn_exp2f((top - most) * a.scale);
             total *= shrink;
 #pragma unroll
             for (int t = 0; t < DT; ++t) acc[t] *= shrink;
+            top = most, limit = most + 8.f * a.per_scale;
+            base = most == kNone ? 0.f : most * a.scale - 7.f;
+        }
 #pragma unroll
-            for (int step = 0; step < 4; ++step) {
-                Frag w;
+        for (int step = 0; step < 4; ++step) {
+            Frag w;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[step / 2][8 * (step & 1) + e], a.scale, -base));
-                    total += p;
-                    w.h[e] = (_Float16)p;
+            for (int e = 0; e < 8; ++e) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[step / 2][8 * (step & 1) + e], a.scale, -base));
+                total += p;
+                w.h[e] = (_Float16)p;
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                Frag v;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int r = 16 * step + 8 * half + 4 * g + ((lane >> 2) & 3);
+                    const int c = 4 * t + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+                    const uint8_t *p = vs + r * (D * 2) + 16 * (c ^ value_swap(r)) + 8 * (lane & 1);
+                    v.s[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
                 }
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    Frag v;
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const int r = 16 * step + 8 * half + 4 * g + ((lane >> 2) & 3);
-                        const int c = 4 * t + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-                        const uint8_t *p = vs + r * (D * 2) + 16 * (c ^ value_swap(r)) + 8 * (lane & 1);
-                        v.s[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
-                    }
-                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v.v, w.v, acc[t], 0, 0, 0);
-                }
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v.v, w.v, acc[t], 0, 0, 0);
             }
         }
     }
+    for (int i = mine; i < n_tiles; ++i) turn(i);        // tiles that only later rows see
     total += __shfl_xor(total, 32, 64);
     if (row >= nq) return;
     const float norm = total > 0.f ? 1.f / total : 0.f;
@@ -231,7 +253,7 @@ hipError_t launch_attn_prefill(const void *Q, int64_t ldq, const void *K, int64_
     a.cu_q = cu_q, a.cu_k = cu_k;
     a.n_seqs = (int)n_seqs, a.tokens_q = (int)T_q, a.tokens_k = (int)T_k;
     a.heads = (int)n_heads, a.kv = (int)kv, a.tiles = (int)(attn_prefill_workgroups(T_q, n_seqs, n_heads) / n_heads);
-    a.causal = causal, a.scale = scale * 1.4426950408889634f;
+    a.causal = causal, a.scale = scale * 1.4426950408889634f, a.per_scale = 1.f / a.scale;
     a.o = static_cast<_Float16 *>(O), a.ldo = ldo;
     return dim == 128 ? launch_dim<128>(a, st) : launch_dim<64>(a, st);
 }
