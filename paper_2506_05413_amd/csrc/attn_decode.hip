@@ -65,16 +65,6 @@ struct Decode {
 __device__ __forceinline__ int length_of(const Decode &a, int b) { return (int)min((int64_t)max(a.lens[b], 0), a.max_len); }
 __device__ __forceinline__ int rounds_of(const Decode &a, int b) { return b < a.n_seqs ? (length_of(a, b) + kRound - 1) / kRound : 0; }
 
-// sum over the lanes up to this one
-__device__ __forceinline__ int scan_of_wave(int v)
-{
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);           // row_shr 1, 2, 4, 8 inside rows of 16,
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);          // the last lane of a row to the next row,
-    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);    // that of the first half to the second
-}
 // rounds in a share
 __device__ __forceinline__ int share_size(const Decode &a, int lane)
 {

@@ -2,28 +2,47 @@
 //
 //   o_i = sum_j softmax(scale q_i . k_j) v_j      over the keys j of row i's own sequence, j <= i + (keys - queries) if causal
 //
-// Bound by the matrix pipe and the exponentials beside it.  A workgroup takes 128 query rows of one head, 32 per wave, and
-// walks over its keys 64 at a time with a running maximum and sum; keys and values come into LDS by DMA, one tile ahead.
-// Both products run on 32 x 32 x 16 matrix instructions with the query row in the columns:
+// A workgroup takes 32 query rows of one head per row wave and walks over their keys 64 at a time with running sums; keys and
+// values come into LDS by DMA, one tile ahead.  Both products run on 32 x 32 x 16 matrix instructions with the query row in the
+// columns:
 //
 //   S^T = K Q^T   lane (m, g) = (lane % 32, lane / 32) gets the scores of row m and of tokens 8 i + 4 g + (0 .. 3)
 //   O^T = V^T P^T its k-index is the token: the eight weights that a lane supplies per instruction are those of tokens
 //                 4 g + (0 .. 3) and 8 + 4 g + (0 .. 3) of sixteen, which it got itself
 //
-// so weights stay in the lane that computed them, a row's maximum and sum are one lane's and its neighbour 32 further, and
-// values are read from LDS with the transposing 8-byte read (four tokens of one column per lane).  Weights are rounded to fp16
-// for the matrix pipe (they are at most 1: half a step is 2^-12 of one); scores, maxima, sums and outputs are held in fp32.
+// so weights stay in the lane that computed them, a row's sum is one lane's and its neighbour 32 further, and values are read
+// from LDS with the transposing 8-byte read (four tokens of one column per lane).
+//
+// Weights are w = exp2(score - base), a row's largest 2^7 when its base is set, and the base is set again only where one might
+// pass 2^16: the sum of a tile's weights, which is needed anyhow, shows it, so that a tile needs no maximum, and most tiles
+// rescale nothing.  They are rounded to fp16 for the matrix pipe (half a step, 2^-11 of each; subnormal below 2^-21 of the largest
+// at least), and the sum in the denominator is that of the rounded ones.  Scores, sums and outputs are held in fp32.
+//
+// What bounds it: long prompts the power the chip may draw (8192 tokens, 32 heads of 128, causal, 128 rows a workgroup: the clock is
+// 1.83 GHz of 2.4 and the matrix pipe busy for half of the cycles; leaving out the exponentials, the reads from LDS or the DMA
+// loads in turn raised the clock and kept the count of cycles), short ones the chain of a row's tiles (1.3 us each with one wave
+// per SIMD).  Hence three shapes of workgroup (us for one prompt of T tokens, 32 heads and 8 key/value heads of 128, causal):
+//                                                                          T = 512   1024   2048   4096   8192
+//   8 row waves        a tile loaded once for 256 rows                        19.2   31.1   56.9    141    518
+//   4 row waves        128 rows, two workgroups on a compute unit             13.9   23.7   47.4    146    537
+//   2 row waves x 2    64 rows; two sets of waves take every other tile       11.6   24.3   65.1    209    772
+//                      and meet in LDS at the end
+// Products interleaved with the weights of the tile before (three tiles in flight) were 9 % slower at 8192 tokens and 15 % at
+// 1024, 64 rows per wave (one wave per SIMD) 30 % slower.
 #include "gemm_common.h"
 
 namespace sr {
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-union Frag { f16x8 v; s16x4 s[2]; u32x4 w; _Float16 h[8]; };
+union Frag { f16x8 v; s16x4 s[2]; f16x2 p[4]; };
 
-constexpr int kRows = 128, kKeys = 64;                   // query rows of a workgroup, keys of a tile
+constexpr int kKeys = 64;                                // keys of a tile
+constexpr int kMatrix = 0x8, kRead = 0x100;              // groups of instructions for the scheduler: matrix products, reads from LDS
 constexpr float kNone = -__builtin_inff();
 
 struct Prefill {
@@ -32,40 +51,78 @@ struct Prefill {
     const int32_t *cu_q, *cu_k;
     int n_seqs, tokens_q, tokens_k;
     int heads, kv, tiles;                                // tiles: of query rows, an upper bound
+    int at_once;                                         // tiles whose workgroups fill half of the places
     int causal;
-    float scale, per_scale;                              // times log2(e); its reciprocal
+    float scale;                                         // times log2(e)
     _Float16 *o;
     int64_t ldo;
 };
 
-// where sequence i of a packed batch lies; ends that do not fit are cut, never followed
-__device__ __forceinline__ void span(const int32_t *cu, int i, int tokens, int &begin, int &length)
+// where a sequence of a packed batch lies; ends that do not fit are cut, never followed
+__device__ __forceinline__ void span(int from, int to, int tokens, int &begin, int &length)
 {
-    begin = min(max(cu[i], 0), tokens);
-    length = min(max(cu[i + 1], begin), tokens) - begin;
+    begin = min(max(from, 0), tokens);
+    length = min(max(to, begin), tokens) - begin;
 }
 
-// the sequence that holds the tile-th tile of query rows, and which of its tiles that is; false behind the last
-__device__ __forceinline__ bool find_tile(const Prefill &a, int tile, int lane, int &seq, int &local)
+// a tile of query rows: its sequence's queries and keys, and its number among that sequence's tiles
+struct Place { int q0, nq, k0, nk, local; };
+
+__device__ __forceinline__ void take(Place &p, int lane_of, int q0, int nq, int k0, int nk)
 {
+    p.q0 = __builtin_amdgcn_readlane(q0, lane_of), p.nq = __builtin_amdgcn_readlane(nq, lane_of);
+    p.k0 = __builtin_amdgcn_readlane(k0, lane_of), p.nk = __builtin_amdgcn_readlane(nk, lane_of);
+}
+
+// The tile-th tile of rows of the batch, those with the most keys first; false behind the last.  A lane looks at a sequence.
+// (Nine prompts of 26 .. 541 tokens: 29.3 -> 25.7 us.)  Up to 64 sequences: tile i of a sequence that has `ahead` more keys than queries is on level i + 1 + ahead / ROWS, and a level
+// is found by bisection over the number of tiles above it.  Where every workgroup has its place at once (`at_once` tiles are
+// half of the places), the second half of them is dealt out from the other end, so that a compute unit's two workgroups are a
+// long and a short one (one prompt of 2048 tokens, 32 heads of 128: 48.6 -> 47.4 us).  More sequences: the last one's last first.
+template <int ROWS> __device__ __forceinline__ bool find_tile(const Prefill &a, int tile, int lane, Place &p)
+{
+    if (a.n_seqs <= 64) {
+        const int s = min(lane, a.n_seqs - 1);
+        const int q_from = a.cu_q[s], q_to = a.cu_q[s + 1], k_from = a.cu_k[s], k_to = a.cu_k[s + 1];
+        int q0, nq, k0, nk;
+        span(q_from, q_to, a.tokens_q, q0, nq);
+        span(k_from, k_to, a.tokens_k, k0, nk);
+        const int n = lane < a.n_seqs ? (nq + ROWS - 1) / ROWS : 0;
+        const int ahead = max(nk - nq, 0) / ROWS;
+        auto above = [&](int level) { return __builtin_amdgcn_readlane(scan_of_wave(min(max(ahead + n - level, 0), n)), 63); };
+        const int all = above(0);
+        if (tile >= all) return false;
+        if (all <= 2 * a.at_once && tile >= a.at_once) tile = all - 1 - (tile - a.at_once);
+        int low = 0, high = (a.tokens_k > a.tokens_q ? a.tokens_k : a.tokens_q) / ROWS + 1;   // above(low) > tile >= above(high)
+        while (high - low > 1) {
+            const int mid = low + (high - low) / 2;
+            if (above(mid) > tile) low = mid;
+            else high = mid;
+        }
+        // the tile is on level `high`
+        const int rank = tile - above(high);
+        const bool here = high > ahead && high <= ahead + n;
+        const unsigned long long mask = __ballot(here);
+        const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+        const int at = __builtin_ctzll(__ballot(here && before == rank));
+        take(p, at, q0, nq, k0, nk);
+        p.local = high - 1 - __builtin_amdgcn_readlane(ahead, at);
+        return true;
+    }
+    tile = a.tiles - 1 - tile;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
-        int n = 0;
-        if (s0 + lane < a.n_seqs) {
-            int begin, length;
-            span(a.cu_q, s0 + lane, a.tokens_q, begin, length);
-            n = (length + kRows - 1) / kRows;
-        }
-        int upto = n;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int other = __shfl_up(upto, d, 64);
-            upto += lane >= d ? other : 0;
-        }
+        const int s = min(s0 + lane, a.n_seqs - 1);
+        const int q_from = a.cu_q[s], q_to = a.cu_q[s + 1], k_from = a.cu_k[s], k_to = a.cu_k[s + 1];
+        int q0, nq, k0, nk;
+        span(q_from, q_to, a.tokens_q, q0, nq);
+        span(k_from, k_to, a.tokens_k, k0, nk);
+        const int n = s0 + lane < a.n_seqs ? (nq + ROWS - 1) / ROWS : 0;
+        const int upto = scan_of_wave(n);
         const unsigned long long past = __ballot(upto > tile);
         if (past) {
             const int at = __builtin_ctzll(past);
-            seq = s0 + at;
-            local = __builtin_amdgcn_readfirstlane(tile - __shfl(upto - n, at, 64));
+            take(p, at, q0, nq, k0, nk);
+            p.local = tile - __builtin_amdgcn_readlane(upto - n, at);
             return true;
         }
         tile -= __builtin_amdgcn_readlane(upto, 63);
@@ -73,89 +130,103 @@ __device__ __forceinline__ bool find_tile(const Prefill &a, int tile, int lane, 
     return false;
 }
 
-template <int D> __global__ __launch_bounds__(256, 2) void attn_prefill_kernel(Prefill a)
+// SETS sets of waves, each with every SETS-th tile of keys
+template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2) void attn_prefill_kernel(Prefill a)
 {
+    constexpr int ROWS = 32 * W;
     constexpr int CH = D / 8;                            // 16-byte chunks of a row
     constexpr uint32_t kTileBytes = kKeys * D * 2;
-    constexpr int DT = D / 32, LOADS = kKeys * CH / 256; // column tiles; DMA loads of a wave per operand
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;   // [2][keys, values]
+    constexpr int DT = D / 32, LOADS = kKeys * CH / (64 * W);    // column tiles; DMA loads of a wave per operand
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];   // per set: [2][keys, values]
     const int lane = threadIdx.x & 63, m = lane & 31, g = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % W), set = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / W);
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem + set * 4 * kTileBytes;
+    const uint8_t *tiles = smem + set * 4 * kTileBytes;
+    // neighbouring workgroups take different key/value heads: an XCD, every eighth of them, keeps few heads' keys in its L2
     const uint32_t x = blockIdx.x % (uint32_t)a.heads;
     const int kvh = (int)(x % (uint32_t)a.kv), head = kvh * (a.heads / a.kv) + (int)(x / (uint32_t)a.kv);
-    int seq, local;
-    if (!find_tile(a, a.tiles - 1 - (int)(blockIdx.x / (uint32_t)a.heads), lane, seq, local)) return;
-    int q0, nq, k0, nk;
-    span(a.cu_q, seq, a.tokens_q, q0, nq);
-    span(a.cu_k, seq, a.tokens_k, k0, nk);
-    q0 = __builtin_amdgcn_readfirstlane(q0), nq = __builtin_amdgcn_readfirstlane(nq);
-    k0 = __builtin_amdgcn_readfirstlane(k0), nk = __builtin_amdgcn_readfirstlane(nk);
-    const int r0 = local * kRows, shift = nk - nq;
-    const int end = a.causal ? min(nk, min(r0 + kRows, nq) + shift) : nk;              // keys that any row sees
+    Place p;
+    if (!find_tile<ROWS>(a, (int)(blockIdx.x / (uint32_t)a.heads), lane, p)) return;
+    const int r0 = p.local * ROWS, shift = p.nk - p.nq;
+    const int end = a.causal ? min(p.nk, min(r0 + ROWS, p.nq) + shift) : p.nk;         // keys that any row sees
     const int w0 = r0 + 32 * wave, row = w0 + m;
-    const int wend = a.causal ? min(nk, min(w0 + 32, nq) + shift) : nk;                // .. of this wave
-    const int rend = a.causal ? min(nk, row + shift + 1) : nk;                         // .. of this lane's row
-    const int whole = a.causal ? min(nk, w0 + shift + 1) : nk;                         // keys that every row of the wave sees
-
-    Frag q[D / 16];
-    {
-        const _Float16 *src = a.q + (int64_t)(q0 + min(row, nq - 1)) * a.ldq + (int64_t)head * D + 8 * g;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) q[i].v = *reinterpret_cast<const f16x8 *>(src + 16 * i);
-    }
-    f32x16 acc[DT];
-#pragma unroll
-    for (int t = 0; t < DT; ++t) acc[t] = 0.f;
-    // Weights are exp2(score - base), a row's largest about 2^7 when base is set, and base is set again only where one would pass
-    // 2^15: fp16 has room for that, its subnormals begin 2^-21 below the largest, and most tiles rescale nothing.
-    float top = kNone, limit = kNone, base = 0.f, total = 0.f;
+    const int wend = w0 >= p.nq ? 0 : a.causal ? min(p.nk, min(w0 + 32, p.nq) + shift) : p.nk;   // .. of this wave
+    const int rend = a.causal ? min(p.nk, row + shift + 1) : p.nk;                     // .. of this lane's row
+    const int whole = a.causal ? min(p.nk, w0 + shift + 1) : p.nk;                     // keys that every row of the wave sees
 
     // Tiles lie in LDS by rows, their chunks swapped so that the lanes that read at once meet every bank: keys, read 32 rows
     // of one chunk at a time, by row; values, read 4 rows of four neighbouring chunks, by row in steps of four chunks.
-    const uint8_t *kb = reinterpret_cast<const uint8_t *>(a.k + (int64_t)k0 * a.ldk + (int64_t)kvh * D);
-    const uint8_t *vb = reinterpret_cast<const uint8_t *>(a.v + (int64_t)k0 * a.ldv + (int64_t)kvh * D);
+    const uint8_t *kb = reinterpret_cast<const uint8_t *>(a.k + (int64_t)p.k0 * a.ldk + (int64_t)kvh * D);
+    const uint8_t *vb = reinterpret_cast<const uint8_t *>(a.v + (int64_t)p.k0 * a.ldv + (int64_t)kvh * D);
     auto key_swap = [](int r) { return D == 128 ? r & 15 : (r >> 1) & 7; };
     auto value_swap = [](int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; };
     uint32_t k_off[LOADS], v_off[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int at = (i * 4 + wave) * 64 + lane, r = at / CH, c = at % CH;
+        const int at = (i * W + wave) * 64 + lane, r = at / CH, c = at % CH;
         k_off[i] = r * (uint32_t)(a.ldk * 2) + 16 * (c ^ key_swap(r));
         v_off[i] = r * (uint32_t)(a.ldv * 2) + 16 * (c ^ value_swap(r));
     }
     auto load = [&](int t0, int slot) {
         const uint8_t *kt = kb + (int64_t)t0 * a.ldk * 2, *vt = vb + (int64_t)t0 * a.ldv * 2;
         const uint32_t to = lds + slot * 2 * kTileBytes + wave * 1024;
-        if (t0 + kKeys <= nk) {
+        if (t0 + kKeys <= p.nk) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                dma16(kt, k_off[i], to + 4096 * i);
-                dma16(vt, v_off[i], to + 4096 * i + kTileBytes);
+                dma16(kt, k_off[i], to + W * 1024 * i);
+                dma16(vt, v_off[i], to + W * 1024 * i + kTileBytes);
             }
         } else {                                         // rows past the end: the last one again
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                const int r = ((i * 4 + wave) * 64 + lane) / CH;
-                const uint32_t over = (uint32_t)max(r - (nk - 1 - t0), 0);
-                dma16(kt, k_off[i] - over * (uint32_t)(a.ldk * 2), to + 4096 * i);
-                dma16(vt, v_off[i] - over * (uint32_t)(a.ldv * 2), to + 4096 * i + kTileBytes);
+                const int r = ((i * W + wave) * 64 + lane) / CH;
+                const uint32_t over = (uint32_t)max(r - (p.nk - 1 - t0), 0);
+                dma16(kt, k_off[i] - over * (uint32_t)(a.ldk * 2), to + W * 1024 * i);
+                dma16(vt, v_off[i] - over * (uint32_t)(a.ldv * 2), to + W * 1024 * i + kTileBytes);
             }
         }
     };
-
     const int n_tiles = end > 0 ? (end + kKeys - 1) / kKeys : 0, mine = wend > 0 ? (wend + kKeys - 1) / kKeys : 0;
-    // the tile that was asked for a round ago is there, and everybody is done with the slot of the next one
-    auto turn = [&](int i) {
+    const int rounds = (n_tiles + SETS - 1) / SETS;
+    if (set < n_tiles) load(set * kKeys, 0);
+
+    Frag q[D / 16];
+    {
+        const _Float16 *src = a.q + (int64_t)(p.q0 + min(row, p.nq - 1)) * a.ldq + (int64_t)head * D + 8 * g;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) q[i].v = *reinterpret_cast<const f16x8 *>(src + 16 * i);
+    }
+    // have them here: a wait for them inside the loop below would be one for everything that is in flight there
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(q[i].v));
+    f32x16 acc[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] = 0.f;
+    float top = kNone, base = 0.f, limit = -1.f, total = 0.f;
+
+    // what was asked for a round ago is there, and everybody is done with the slot that is asked for now
+    auto turn = [&](int round) {
         wait_vmcnt<0>();
         barrier_nofence();
-        if (i + 1 < n_tiles) load((i + 1) * kKeys, (i + 1) & 1);
+        const int next = (round + 1) * SETS + set;
+        if (next < n_tiles) load(next * kKeys, (round + 1) & 1);
     };
-    if (n_tiles) load(0, 0);
-    for (int i = 0; i < mine; ++i) {
-        const int t0 = i * kKeys;
-        turn(i);
-        const uint8_t *ks = smem + (i & 1) * 2 * kTileBytes, *vs = ks + kTileBytes;
+    int round = 0;
+    for (; round * SETS + set < mine; ++round) {
+        turn(round);
+        const int t0 = (round * SETS + set) * kKeys;
+        const uint8_t *ks = tiles + (round & 1) * 2 * kTileBytes, *vs = ks + kTileBytes;
+        auto value = [&](int step, int t) {
+            Frag v;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int r = 16 * step + 8 * half + 4 * g + ((lane >> 2) & 3);
+                const int c = 4 * t + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+                const uint8_t *from = vs + r * (D * 2) + 16 * (c ^ value_swap(r)) + 8 * (lane & 1);
+                v.s[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)from);
+            }
+            return v;
+        };
         f32x16 s[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -168,6 +239,14 @@ template <int D> __global__ __launch_bounds__(256, 2) void attn_prefill_kernel(P
                 s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k.v, q[d].v, s[u], 0, 0, 0);
             }
         }
+        // six keys' reads ahead of the products, one more with each
+        __builtin_amdgcn_sched_group_barrier(kRead, 6, 0);
+#pragma unroll
+        for (int i = 0; i < D / 8 - 6; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 6, 0);
         if (t0 + kKeys > whole) {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -175,48 +254,83 @@ template <int D> __global__ __launch_bounds__(256, 2) void attn_prefill_kernel(P
                 for (int e = 0; e < 16; ++e)
                     if (t0 + 32 * u + 8 * (e / 4) + 4 * g + (e & 3) >= rend) s[u][e] = kNone;
         }
-        float most = kNone;
+        Frag w[4];                                       // of 16 tokens each
+        float sum;
+        auto weigh = [&] {
+            sum = 0.f;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[u][e]);
-        if (!__all(most <= limit)) {
-            most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), top);
-            const float shrink = most == kNone ? 1.f : __builtin_amdgcn_exp2f((top - most) * a.scale);
-            total *= shrink;
-#pragma unroll
-            for (int t = 0; t < DT; ++t) acc[t] *= shrink;
-            top = most, limit = most + 8.f * a.per_scale;
-            base = most == kNone ? 0.f : most * a.scale - 7.f;
-        }
-#pragma unroll
-        for (int step = 0; step < 4; ++step) {
-            Frag w;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(s[step / 2][8 * (step & 1) + e], a.scale, -base));
-                total += p;
-                w.h[e] = (_Float16)p;
-            }
-#pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                Frag v;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int r = 16 * step + 8 * half + 4 * g + ((lane >> 2) & 3);
-                    const int c = 4 * t + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-                    const uint8_t *p = vs + r * (D * 2) + 16 * (c ^ value_swap(r)) + 8 * (lane & 1);
-                    v.s[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
+                for (int e = 0; e < 16; e += 2) {
+                    f16x2 &pair = w[2 * u + e / 8].p[e / 2 % 4];
+                    pair = f16x2{(_Float16)__builtin_amdgcn_exp2f(fmaf(s[u][e], a.scale, -base)), (_Float16)__builtin_amdgcn_exp2f(fmaf(s[u][e + 1], a.scale, -base))};
+                    sum = __builtin_amdgcn_fdot2(pair, f16x2{(_Float16)1.f, (_Float16)1.f}, sum, false);
                 }
-                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v.v, w.v, acc[t], 0, 0, 0);
+        };
+        weigh();
+        if (!__all(sum <= limit)) {                      // (a weight beyond fp16 is infinite, and so is the sum)
+            float most = kNone;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) most = fmaxf(most, s[u][e]);
+            most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), top);
+            if (most != kNone) {
+                const float now = most * a.scale - 7.f, shrink = top == kNone ? 1.f : __builtin_amdgcn_exp2f(base - now);
+                total *= shrink;
+#pragma unroll
+                for (int t = 0; t < DT; ++t) acc[t] *= shrink;
+                base = now, top = most, limit = 32768.f;
             }
+            weigh();
         }
+        total += sum;
+#pragma unroll
+        for (int step = 0; step < 4; ++step)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(step, t).v, w[step].v, acc[t], 0, 0, 0);
+        // eight reads (of four products) ahead, two more with each
+        __builtin_amdgcn_sched_group_barrier(kRead, 8, 1);
+#pragma unroll
+        for (int i = 0; i < 4 * DT - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(kRead, 2, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 1);
     }
-    for (int i = mine; i < n_tiles; ++i) turn(i);        // tiles that only later rows see
+    for (; round < rounds; ++round) turn(round);         // tiles that only other waves need
+
+    if constexpr (SETS == 2) {
+        // the second set hands over what it has: 16 bytes of a lane beside those of the next
+        barrier_nofence();
+        f32x4 *area = reinterpret_cast<f32x4 *>(smem + wave * (D / 8 * 1024));
+        float2 *state = reinterpret_cast<float2 *>(smem + W * (D / 8 * 1024)) + wave * 64;
+        if (set == 1) {
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) area[(4 * t + e) * 64 + lane] = f32x4{acc[t][4 * e], acc[t][4 * e + 1], acc[t][4 * e + 2], acc[t][4 * e + 3]};
+            state[lane] = make_float2(top == kNone ? kNone : base, total);
+        }
+        __syncthreads();
+        if (set == 1) return;
+        const float2 other = state[lane];
+        const float own = top == kNone ? kNone : base, both = fmaxf(own, other.x);
+        const float mine_by = own == kNone ? 0.f : __builtin_amdgcn_exp2f(own - both), other_by = other.x == kNone ? 0.f : __builtin_amdgcn_exp2f(other.x - both);
+        total = total * mine_by + other.y * other_by;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f32x4 y = area[(4 * t + e) * 64 + lane];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[t][4 * e + r] = acc[t][4 * e + r] * mine_by + y[r] * other_by;
+            }
+    }
     total += __shfl_xor(total, 32, 64);
-    if (row >= nq) return;
+    if (row >= p.nq) return;
     const float norm = total > 0.f ? 1.f / total : 0.f;
-    _Float16 *dst = a.o + (int64_t)(q0 + row) * a.ldo + (int64_t)head * D + 4 * g;
+    _Float16 *dst = a.o + (int64_t)(p.q0 + row) * a.ldo + (int64_t)head * D + 4 * g;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -228,20 +342,21 @@ template <int D> __global__ __launch_bounds__(256, 2) void attn_prefill_kernel(P
         }
 }
 
-template <int D> hipError_t launch_dim(const Prefill &a, hipStream_t st)
+// tiles of rows, at most: every sequence may end inside one
+int64_t tiles_of(int64_t T_q, int64_t n_seqs, int64_t rows) { return T_q / rows + (n_seqs < T_q ? n_seqs : T_q); }
+
+template <int D, int W, int SETS> hipError_t launch_dim(Prefill a, int64_t n_seqs, hipStream_t st)
 {
-    constexpr int bytes = 4 * kKeys * D * 2;
-    if (hipError_t e = allow_dynamic_lds<attn_prefill_kernel<D>>(bytes); e != hipSuccess) return e;
-    hipLaunchKernelGGL((attn_prefill_kernel<D>), dim3((unsigned)((int64_t)a.tiles * a.heads)), dim3(256), bytes, st, a);
+    constexpr int bytes = SETS * 4 * kKeys * D * 2;
+    if (hipError_t e = allow_dynamic_lds<attn_prefill_kernel<D, W, SETS>>(bytes); e != hipSuccess) return e;
+    a.tiles = (int)tiles_of(a.tokens_q, n_seqs, 32 * W);
+    hipLaunchKernelGGL((attn_prefill_kernel<D, W, SETS>), dim3((unsigned)((int64_t)a.tiles * a.heads)), dim3(64 * W * SETS), bytes, st, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t attn_prefill_workgroups(int64_t T_q, int64_t n_seqs, int64_t n_heads)
-{
-    return (T_q / kRows + (n_seqs < T_q ? n_seqs : T_q)) * n_heads;      // every sequence may end inside a tile
-}
+int64_t attn_prefill_workgroups(int64_t T_q, int64_t n_seqs, int64_t n_heads) { return tiles_of(T_q, n_seqs, 64) * n_heads; }
 
 hipError_t launch_attn_prefill(const void *Q, int64_t ldq, const void *K, int64_t ldk, const void *V, int64_t ldv,
                                const int32_t *cu_q, const int32_t *cu_k, int64_t n_seqs, int64_t T_q, int64_t T_k, int64_t n_heads,
@@ -252,10 +367,17 @@ hipError_t launch_attn_prefill(const void *Q, int64_t ldq, const void *K, int64_
     a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
     a.cu_q = cu_q, a.cu_k = cu_k;
     a.n_seqs = (int)n_seqs, a.tokens_q = (int)T_q, a.tokens_k = (int)T_k;
-    a.heads = (int)n_heads, a.kv = (int)kv, a.tiles = (int)(attn_prefill_workgroups(T_q, n_seqs, n_heads) / n_heads);
-    a.causal = causal, a.scale = scale * 1.4426950408889634f, a.per_scale = 1.f / a.scale;
+    a.heads = (int)n_heads, a.kv = (int)kv;
+    a.causal = causal, a.scale = scale * 1.4426950408889634f;
     a.o = static_cast<_Float16 *>(O), a.ldo = ldo;
-    return dim == 128 ? launch_dim<128>(a, st) : launch_dim<64>(a, st);
+    // Two sets of waves while the workgroups of 64 rows have their places at once; 256 rows where there are two rounds of such
+    // workgroups of long sequences (heads of 64 gain nothing: 4096 tokens, 32 heads 93 us for 91).
+    const int64_t units = compute_units();
+    a.at_once = 0;
+    if (T_q * n_heads <= 64 * units * (128 / dim)) return dim == 128 ? launch_dim<128, 2, 2>(a, n_seqs, st) : launch_dim<64, 2, 2>(a, n_seqs, st);
+    if (dim == 128 && T_q * n_heads >= 2 * 256 * units && T_q >= 1024 * n_seqs) return launch_dim<128, 8, 1>(a, n_seqs, st);
+    a.at_once = (int)((units + n_heads - 1) / n_heads);
+    return dim == 128 ? launch_dim<128, 4, 1>(a, n_seqs, st) : launch_dim<64, 4, 1>(a, n_seqs, st);
 }
 
 }  // namespace sr

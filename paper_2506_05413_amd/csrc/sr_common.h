@@ -62,6 +62,17 @@ __device__ __forceinline__ float max_of_wave(float v)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// sum over the lanes up to this one
+__device__ __forceinline__ int scan_of_wave(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);           // row_shr 1, 2, 4, 8 inside rows of 16,
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);          // the last lane of a row to the next row,
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);    // that of the first half to the second
+}
+
 // ---- tuning knobs (host) ---------------------------------------------------------------
 // Process-wide overrides of the dispatch heuristics, set through sr_tune_set (include/smoothrot.h): the tests
 // use them to run every kernel on every shape, tuning runs to compare variants inside one process.  A knob that

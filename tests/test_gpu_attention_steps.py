@@ -52,7 +52,7 @@ class Server:
         return self.sr.sr_rope_kv_append(x[:, :H * D], x[:, H * D:(H + KV) * D], x[:, (H + KV) * D:], pos, slots, self.cos_sin, self.cache, hadamard=True)
 
     def check(self, got, q, of, what, rounded):
-        """rounded: keys and values went through fp16 on their way out of the cache."""
+        """rounded: sr_attn_prefill on keys and values that went through fp16 on their way out of the cache."""
         got = got.cpu().numpy().reshape(-1, H, D)
         for b in range(2):
             rows = of == b
@@ -64,7 +64,7 @@ class Server:
                     ks, vs = np.abs(k), np.abs(v)
                 qq = q[rows, h].astype(np.float64)
                 o, p, s = ao.attend(qq, k, v, 1 / np.sqrt(D), ao.causal(n, m))
-                check_attention(got[rows, h], o, attention_bound(qq, ks, v, vs, o, p, s, 1 / np.sqrt(D)), "%s sequence %d head %d" % (what, b, h))
+                check_attention(got[rows, h], o, attention_bound(qq, ks, v, vs, o, p, s, 1 / np.sqrt(D), rounded_total=rounded), "%s sequence %d head %d" % (what, b, h))
 
 
 def test_chunks_of_prompts_then_tokens(gpu):

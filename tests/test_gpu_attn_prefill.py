@@ -34,7 +34,7 @@ def check(got, q, k, v, nq, nk, causal, scale, what=""):
         for h in range(H if n else 0):
             qq, kk, vv = q[i:i + n, h].astype(np.float64), k[j:j + m, h * KV // H].astype(np.float64), v[j:j + m, h * KV // H].astype(np.float64)
             o, p, sc = ao.attend(qq, kk, vv, scale, seen)
-            bound = attention_bound(qq, np.abs(kk), vv, np.abs(vv), o, p, sc, scale)
+            bound = attention_bound(qq, np.abs(kk), vv, np.abs(vv), o, p, sc, scale, rounded_total=True)
             worst = max(worst, check_attention(got[i:i + n, h], o, bound, "%s sequence %d (%d queries, %d keys) head %d" % (what, s, n, m, h)))
         i, j = i + n, j + m
     return worst
@@ -78,6 +78,20 @@ def test_other_numbers_of_keys(gpu, d, causal):
 def test_one_prompt(gpu, T, H, KV, d):
     q, k, v = make([T], [T], H, KV, d, seed=T)
     check(run(gpu, q, k, v, [T], [T]), q, k, v, [T], [T], True, 1 / np.sqrt(d))
+
+
+@pytest.mark.parametrize("nq,nk,H,KV,d", [([300], [300], 12, 3, 128), ([700, 650, 900, 80], [700, 1400, 900, 33], 24, 6, 128), ([2500], [2500], 56, 1, 128),
+                                          ([1100, 1500], [1100, 1700], 60, 2, 128), ([700, 10, 650], [800, 10, 650], 40, 4, 64), ([140] * 70, [150] * 70, 8, 8, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_every_shape_of_workgroup(gpu, nq, nk, H, KV, d, causal):
+    """Few rows (two sets of waves over the keys), more of them (128 rows a workgroup, with and without all of them at once, and
+    more sequences than a wave looks at), and long sequences (256)."""
+    print("case prefill", len(nq), sum(nq), H, KV, d, causal, flush=True)
+    q, k, v = make(nq, nk, H, KV, d, seed=sum(nq))
+    got = run(gpu, q, k, v, nq, nk, causal)
+    few = [0, H // 2, H - 1]                             # of the heads
+    at = [h * KV // H for h in few]
+    check(got[:, few], q[:, few], k[:, at], v[:, at], nq, nk, causal, 1 / np.sqrt(d))
 
 
 @pytest.mark.parametrize("scale", [1e-4, 0.7, 4.0])
