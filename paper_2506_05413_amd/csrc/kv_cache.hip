@@ -7,7 +7,8 @@
 // Every product, sum and quotient is rounded on its own (no fused multiply-add): keys are rounded to fp16 and values next to
 // a rounding boundary take the code that the formula in fp32 gives, whoever evaluates it.
 //
-// Pure streaming.  Eight values (16 bytes) per lane, D / 8 lanes per row, a row being one head of one token, query, key or
+// Bound by its bytes where there are many tokens (16384 with 32 query heads and 8 key/value heads of 128, 4 bits: 363 MB in 80 us,
+// 4.5 TB/s; 2047 with the transform 14 us, 3.3 TB/s), else by the launch (one token 2.5 us).  Eight values (16 bytes) per lane, D / 8 lanes per row, a row being one head of one token, query, key or
 // value; the head's other half, the butterflies and the range of a row are exchanged between those lanes with operand
 // permutations, without LDS.
 #include "sr_common.h"
@@ -28,14 +29,29 @@ template <int MASK, typename T> __device__ __forceinline__ T lane_xor(T v)
     else return lane_perm<0x128>(v);                                              // rotation by 8 of 16
 }
 
+// Lanes with bit MASK clear get own + other, the others own - other, the negative of what the transform says: one fused
+// multiply-add of the partner's value by 1 or -1, which rounds like the sum.  Partners of later steps carry the same signs, so
+// that all of them come to one sign per lane at the end.  (Spelled out: from the exchange and the multiply-add the compiler makes
+// a move and an operation per value.  A lane exchange of a register needs two cycles after it was written.)
 template <int MASK> __device__ __forceinline__ void butterfly(float (&v)[8], int lane)
 {
-    const uint32_t flip = lane & MASK ? 0x80000000u : 0u;
+    const float sign = lane & MASK ? -1.f : 1.f;
+#define SR_STEP(CTRL)                                                                                                              \
+    asm("s_nop 1\n\t"                                                                                                              \
+        "v_fmac_f32_dpp %0, %0, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %1, %1, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t" \
+        "v_fmac_f32_dpp %2, %2, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %3, %3, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t" \
+        "v_fmac_f32_dpp %4, %4, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %5, %5, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\t" \
+        "v_fmac_f32_dpp %6, %6, %8 " CTRL " row_mask:0xf bank_mask:0xf\n\tv_fmac_f32_dpp %7, %7, %8 " CTRL " row_mask:0xf bank_mask:0xf"     \
+        : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7])                             \
+        : "v"(sign))
+    if constexpr (MASK == 1) SR_STEP("quad_perm:[1,0,3,2]");
+    else if constexpr (MASK == 2) SR_STEP("quad_perm:[2,3,0,1]");
+    else if constexpr (MASK == 8) SR_STEP("row_ror:8");
+    else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float other = lane_xor<MASK>(v[e]);
-        v[e] = other + __uint_as_float(__float_as_uint(v[e]) ^ flip);
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(lane_xor<4>(v[e]), sign, v[e]);
     }
+#undef SR_STEP
 }
 
 // v <- v H / sqrt(D) over the 8 values of each of the D / 8 lanes
@@ -55,37 +71,43 @@ template <int D> __device__ __forceinline__ void hadamard_row(float (&v)[8], int
     butterfly<2>(v, lane);
     butterfly<4>(v, lane);
     if constexpr (D == 128) butterfly<8>(v, lane);
-    constexpr float norm = D == 128 ? 0.08838834764831845f : 0.125f;
+    const float norm = (__popc(lane) & 1 ? -1.f : 1.f) * (D == 128 ? 0.08838834764831845f : 0.125f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = v[e] * norm;
 }
 
-template <int D, bool PAIRS> __device__ __forceinline__ void rotate_row(float (&v)[8], const Eight &x, const float *row, int lane)
+// a lane's share of a position's angles: those of its eight values (PAIRS: four pairs)
+template <bool PAIRS> struct Angles {
+    static constexpr int N = PAIRS ? 1 : 2;
+    f32x4 c[N], s[N];
+};
+template <int D, bool PAIRS> __device__ __forceinline__ Angles<PAIRS> angles_at(const float *row, int lane)
+{
+    Angles<PAIRS> a;
+    const int first = PAIRS ? 4 * lane : 8 * (lane & (D / 16 - 1));
+#pragma unroll
+    for (int i = 0; i < a.N; ++i) {
+        a.c[i] = *reinterpret_cast<const f32x4 *>(row + first + 4 * i);
+        a.s[i] = *reinterpret_cast<const f32x4 *>(row + D / 2 + first + 4 * i);
+    }
+    return a;
+}
+template <int D, bool PAIRS> __device__ __forceinline__ void rotate_row(float (&v)[8], const Eight &x, const Angles<PAIRS> &a, int lane)
 {
 #pragma clang fp contract(off)
     if constexpr (PAIRS) {
-        const f32x4 c = *reinterpret_cast<const f32x4 *>(row + 4 * lane), s = *reinterpret_cast<const f32x4 *>(row + D / 2 + 4 * lane);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float a = v[2 * e], b = v[2 * e + 1];
-            v[2 * e] = a * c[e] - b * s[e];
-            v[2 * e + 1] = b * c[e] + a * s[e];
+            const float p = v[2 * e], q = v[2 * e + 1];
+            v[2 * e] = p * a.c[0][e] - q * a.s[0][e];
+            v[2 * e + 1] = q * a.c[0][e] + p * a.s[0][e];
         }
     } else {
-        const int first = 8 * (lane & (D / 16 - 1));
         Eight p;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p.w[i] = (uint32_t)lane_xor<D / 16>((int)x.w[i]);
-        const uint32_t flip = lane < D / 16 ? 0x80000000u : 0u;
+        for (int i = 0; i < 4; ++i) p.w[i] = (uint32_t)lane_xor<D / 16>((int)x.w[i]) ^ (lane < D / 16 ? 0x80008000u : 0u);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const f32x4 c = *reinterpret_cast<const f32x4 *>(row + first + 4 * q), s = *reinterpret_cast<const f32x4 *>(row + D / 2 + first + 4 * q);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float sine = __uint_as_float(__float_as_uint(s[e]) ^ flip);
-                v[4 * q + e] = v[4 * q + e] * c[e] + __half2float(p.h[4 * q + e]) * sine;
-            }
-        }
+        for (int e = 0; e < 8; ++e) v[e] = v[e] * a.c[e / 4][e % 4] + __half2float(p.h[e]) * a.s[e / 4][e % 4];
     }
 }
 
@@ -104,12 +126,22 @@ template <int D> __device__ __forceinline__ uint32_t quantise_row(const Eight &x
     if constexpr (D == 128) mx = fmaxf(mx, lane_perm<0x140>(mx)), mn = fminf(mn, lane_perm<0x140>(mn));
     const float hi = clip * mx, lo = clip * mn;
     scale = hi == lo ? 1.f : (hi - lo) * (1.f / 15.f);
-    zero = -rintf(lo / scale);
+    // Quotients from the correctly rounded reciprocal y: q = a y, and one step q + (a - q d) y with the exact remainder gives
+    // the correctly rounded a / d (Markstein, 1990); a and d are far from the ends of fp32's range.
+    const float y = 1.f / scale;
+    auto over_scale = [&](float a) {
+        const float q = a * y;
+        return fmaf(fmaf(-q, scale, a), y, q);
+    };
+    zero = -rintf(over_scale(lo));
+    // Adding 1.5 * 2^23 rounds a quotient (below 2^16 in size) to the nearest integer, ties to even, in the low bits.
+    constexpr uint32_t kMagic = 0x4B400000u;
+    const int shift = (int)zero - (int)kMagic;
     uint32_t word = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float c = fminf(fmaxf(rintf(v[e] / scale) + zero, 0.f), 15.f);
-        word |= (uint32_t)c << (4 * e);
+        const int c = (int)__float_as_uint(over_scale(v[e]) + __uint_as_float(kMagic)) + shift;
+        word |= (uint32_t)min(max(c, 0), 15) << (4 * e);
     }
     return word;
 }
@@ -132,14 +164,17 @@ struct Append {
     int64_t ldqo, ldko;
 };
 
+// (One row per group of lanes: two or four, on their way together, were 2 - 8 % slower up to 4096 tokens and 4 % faster at 16384.)
 template <int D, bool I4, bool PAIRS, bool HAD> __global__ __launch_bounds__(256) void rope_kv_append_kernel(Append a)
 {
-    constexpr int LPR = D / 8;
+    constexpr int LPR = D / 8, GROUPS = 256 / LPR;
     const int lane = threadIdx.x & (LPR - 1);
-    const uint32_t row = blockIdx.x * (256u / LPR) + threadIdx.x / LPR;
+    const uint32_t per = a.heads + 2 * a.kv, first = blockIdx.x * (uint32_t)GROUPS, row = first + threadIdx.x / LPR;
     if (row >= a.rows) return;
-    const uint32_t per = a.heads + 2 * a.kv, token = row / per;
-    const int head = (int)(row - token * per);
+    const uint32_t token0 = first / per, rest = row - token0 * per;
+    // (the quotient, 32 at most, is half a row away from the next whole number)
+    const uint32_t on = (uint32_t)(((float)rest + 0.5f) * __builtin_amdgcn_rcpf((float)per)), token = token0 + on;
+    const int head = (int)(rest - on * per);
     const bool is_q = head < a.heads, is_v = head >= a.heads + a.kv;
     const int h = is_q ? head : is_v ? head - a.heads - a.kv : head - a.heads;
     const __half *src = is_q ? a.q + token * a.ldq : is_v ? a.v + token * a.ldv : a.k + token * a.ldk;
@@ -152,11 +187,14 @@ template <int D, bool I4, bool PAIRS, bool HAD> __global__ __launch_bounds__(256
         for (int e = 0; e < 8; ++e) v[e] = __half2float(x.h[e]);
         if (a.table) {
             const int pos = min(max(a.positions[token], 0), a.max_pos - 1);
-            rotate_row<D, PAIRS>(v, x, a.table + (int64_t)pos * D, lane);
+            rotate_row<D, PAIRS>(v, x, angles_at<D, PAIRS>(a.table + (int64_t)pos * D, lane), lane);
         }
         if constexpr (HAD) hadamard_row<D>(v, lane);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x.h[e] = __float2half_rn(v[e]);
+        for (int e = 0; e < 8; ++e) {
+            asm("" : "+v"(v[e]));                        // a number of fp32: the last product is not to be rounded to fp16 at once
+            x.h[e] = __float2half_rn(v[e]);
+        }
     }
     if (is_q) {
         *reinterpret_cast<u32x4 *>(a.qo + token * a.ldqo + (int64_t)h * D + 8 * lane) = x.v;
@@ -189,40 +227,72 @@ struct Gather {
     int64_t ldko, ldvo;
 };
 
-template <int D, bool I4> __global__ __launch_bounds__(256) void kv_gather_kernel(Gather a)
+// N rows per group of lanes, a workgroup's apart: their slots, then their rows, then their values
+template <int D, bool I4, int N> __global__ __launch_bounds__(256) void kv_gather_kernel(Gather a)
 {
 #pragma clang fp contract(off)
-    constexpr int LPR = D / 8;
+    constexpr int LPR = D / 8, GROUPS = 256 / LPR;
     const int lane = threadIdx.x & (LPR - 1);
-    const uint32_t row = blockIdx.x * (256u / LPR) + threadIdx.x / LPR;
-    if (row >= a.rows) return;
-    const uint32_t token = row / (2 * a.kv);
-    const int side = (int)(row - token * (2 * a.kv)), h = side % a.kv;
-    const bool is_v = side >= a.kv;
-    const int64_t slot = a.slots[token];
-    Eight x;
-    x.v = 0u;
-    if (slot >= 0 && slot < a.n_slots) {
-        const int64_t at = (((slot >> a.page_shift) * a.kv + h) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
-        const void *cache = is_v ? a.V : a.K;
-        if constexpr (I4) {
-            const uint32_t word = static_cast<const uint32_t *>(cache)[at * LPR + lane];
-            const float2 p = reinterpret_cast<const float2 *>(is_v ? a.Vp : a.Kp)[at];
+    const uint32_t per = 2 * a.kv, first = blockIdx.x * (uint32_t)(GROUPS * N), token0 = first / per, rest0 = first - token0 * per;
+    const float per_row = __builtin_amdgcn_rcpf((float)per);
+    uint32_t token[N];
+    int side[N];                                         // head, or kv + head; of rows behind the last: the last one's
+    int64_t at[N];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x.h[e] = __float2half_rn(((float)((word >> (4 * e)) & 15u) - p.y) * p.x);
+    for (int k = 0; k < N; ++k) {
+        const uint32_t rest = min(rest0 + GROUPS * k + threadIdx.x / LPR, a.rows - 1 - token0 * per);
+        const uint32_t on = (uint32_t)(((float)rest + 0.5f) * per_row);      // 64 at most, half a row away from a whole number
+        token[k] = token0 + on, side[k] = (int)(rest - on * per);
+        const int64_t slot = a.slots[token[k]];
+        const int h = side[k] < a.kv ? side[k] : side[k] - a.kv;
+        at[k] = slot >= 0 && slot < a.n_slots ? (((slot >> a.page_shift) * a.kv + h) << a.page_shift) + (slot & ((1 << a.page_shift) - 1)) : -1;
+    }
+    uint32_t word[N];
+    float2 params[N];
+    Eight x[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        x[k].v = 0u, word[k] = 0, params[k] = make_float2(0.f, 0.f);
+        if (at[k] < 0) continue;
+        const void *cache = side[k] < a.kv ? a.K : a.V;
+        if constexpr (I4) {
+            word[k] = static_cast<const uint32_t *>(cache)[at[k] * LPR + lane];
+            params[k] = reinterpret_cast<const float2 *>(side[k] < a.kv ? a.Kp : a.Vp)[at[k]];
         } else {
-            x.v = static_cast<const u32x4 *>(cache)[at * LPR + lane];
+            x[k].v = static_cast<const u32x4 *>(cache)[at[k] * LPR + lane];
         }
     }
-    __half *dst = is_v ? a.vo + token * a.ldvo : a.ko + token * a.ldko;
-    *reinterpret_cast<u32x4 *>(dst + (int64_t)h * D + 8 * lane) = x.v;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if constexpr (I4) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float v = ((float)((word[k] >> (4 * e)) & 15u) - params[k].y) * params[k].x;
+                asm("" : "+v"(v));
+                x[k].h[e] = __float2half_rn(v);
+            }
+        }
+        __half *dst = side[k] < a.kv ? a.ko + token[k] * a.ldko + (int64_t)side[k] * D : a.vo + token[k] * a.ldvo + (int64_t)(side[k] - a.kv) * D;
+        *reinterpret_cast<u32x4 *>(dst + 8 * lane) = x[k].v;
+    }
+}
+
+// Two rows per group of lanes from eight workgroups on every compute unit on (16384 tokens of 8 heads of 128, 4 bits: 21.9 ->
+// 19.8 us, 86 MB; four 19.3, but 4096 tokens 6.3 -> 6.7); nothing gained or lost below.
+template <int D, bool I4> hipError_t gather_dim(const Gather &a, hipStream_t st)
+{
+    constexpr unsigned rows = 256 / (D / 8);
+    if (a.rows >= 8 * rows * (unsigned)compute_units()) hipLaunchKernelGGL((kv_gather_kernel<D, I4, 2>), dim3((a.rows + 2 * rows - 1) / (2 * rows)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((kv_gather_kernel<D, I4, 1>), dim3((a.rows + rows - 1) / rows), dim3(256), 0, st, a);
+    return hipGetLastError();
 }
 
 inline int shift_of(int64_t page) { return __builtin_ctzll((unsigned long long)page); }
 
 template <int D, bool I4> hipError_t append_dim(const Append &a, bool pairs, bool had, hipStream_t st)
 {
-    const dim3 grid((unsigned)(((uint64_t)a.rows * (D / 8) + 255) / 256)), block(256);
+    constexpr unsigned rows = 256 / (D / 8);
+    const dim3 grid((a.rows + rows - 1) / rows), block(256);
     if (pairs && had) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, true, true>), grid, block, 0, st, a);
     else if (pairs) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, true, false>), grid, block, 0, st, a);
     else if (had) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, false, true>), grid, block, 0, st, a);
@@ -261,12 +331,8 @@ hipError_t launch_kv_gather(const int64_t *slots, int64_t T, const KvCache &c, v
     a.n_slots = c.pages * c.page_size, a.page_shift = shift_of(c.page_size);
     a.ko = static_cast<__half *>(K_out), a.vo = static_cast<__half *>(V_out);
     a.ldko = ldko, a.ldvo = ldvo;
-    const dim3 grid((unsigned)(((uint64_t)a.rows * (c.dim / 8) + 255) / 256)), block(256);
-    if (c.dim == 128 && c.i4) hipLaunchKernelGGL((kv_gather_kernel<128, true>), grid, block, 0, st, a);
-    else if (c.dim == 128) hipLaunchKernelGGL((kv_gather_kernel<128, false>), grid, block, 0, st, a);
-    else if (c.i4) hipLaunchKernelGGL((kv_gather_kernel<64, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((kv_gather_kernel<64, false>), grid, block, 0, st, a);
-    return hipGetLastError();
+    if (c.dim == 128) return c.i4 ? gather_dim<128, true>(a, st) : gather_dim<128, false>(a, st);
+    return c.i4 ? gather_dim<64, true>(a, st) : gather_dim<64, false>(a, st);
 }
 
 }  // namespace sr
