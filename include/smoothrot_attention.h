@@ -78,7 +78,8 @@ SR_API int sr_kv_gather(const int64_t *slots, int64_t T, const sr_kv_cache *cach
  * Attention of one new token per sequence over its pages:
  *     o = sum_t p_t v_t,  p = softmax(scale * q . k_t)  over the tokens t < seq_lens[b]
  * with the values that the cache stands for (4 bits: (code - z) * d, not rounded); scores, maxima and sums in fp32, weights
- * rounded to fp16 for the product with the values, o rounded once.  The cache is split over its length and joined.
+ * rounded to fp16 for the product with the values, o rounded once.  The tokens of all sequences are dealt out in equal shares and
+ * the parts of a sequence joined, unless the table is narrow or the sequences many; the same call gives the same bits.
  *   Q_f16        fp16 [n_seqs, n_heads * head_dim], row stride ldq
  *   page_table   int32 [n_seqs, max_pages], row stride ld_table: page i holds tokens i * page_size .. of the sequence.  Entries
  *                behind the length are not looked at; the tokens of an entry outside [0, n_pages) are left out.
@@ -88,11 +89,12 @@ SR_API int sr_kv_gather(const int64_t *slots, int64_t T, const sr_kv_cache *cach
  *   O_f16        out, fp16 [n_seqs, n_heads * head_dim], row stride ldo
  *   workspace    sr_attn_decode_workspace_bytes(...) bytes on the device that is current, 256-byte aligned (may be NULL where
  *                that is 0).  Contents need no initialisation; calls that share one must not overlap (captured graphs included).
- * The runs that the cache is cut into follow max_pages * page_size, not the lengths (which are not known on the host): pass a
- * table that is no wider than the longest sequence needs.  max_pages * page_size <= 2^30.
+ * Lengths are not known on the host: whether there are shares (and a workspace) follows n_seqs, the heads, the cache's type and
+ * max_pages * page_size, so a table that is no wider than the longest sequence needs is best.  max_pages * page_size <= 2^30.
+ *   type         of the cache: SR_KV_F16 or SR_KV_I4.  0 for arguments that sr_attn_decode refuses.
  */
 SR_API size_t sr_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,
-                                      int64_t max_pages, int64_t page_size);
+                                      int64_t max_pages, int64_t page_size, int type);
 SR_API int sr_attn_decode(const void *Q_f16, int64_t ldq, int64_t n_seqs, int64_t n_heads, const sr_kv_cache *cache,
                    const int32_t *page_table, int64_t max_pages, int64_t ld_table, const int32_t *seq_lens, float scale,
                    void *O_f16, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
@@ -101,8 +103,8 @@ SR_API int sr_attn_decode(const void *Q_f16, int64_t ldq, int64_t n_seqs, int64_
  * Attention of whole prompts, packed one behind the other:
  *     o_i = sum_j p_j v_j,  p = softmax(scale * q_i . k_j)  over the keys j of row i's own sequence
  * and, if causal, over j <= i + (keys of the sequence - queries of the sequence): the last query sees every key, so that a
- * chunk of a prompt is passed with the keys of the chunks before it in front.  A row that sees no key gives zeros.  Arithmetic
- * as in sr_attn_decode.
+ * chunk of a prompt is passed with the keys of the chunks before it in front.  A row that sees no key gives zeros.  Scores,
+ * maxima and sums in fp32, weights rounded to fp16 and divided by the sum of the rounded ones, o rounded once.
  *   Q_f16          fp16 [T_q, n_heads * head_dim], row stride ldq
  *   K_f16, V_f16   fp16 [T_k, n_kv_heads * head_dim], row strides ldk, ldv (may be NULL with T_k = 0)
  *   cu_q, cu_k     int32 [n_seqs + 1]: sequence s holds rows cu_q[s] .. cu_q[s + 1] - 1 of Q and cu_k[s] .. of K and V (ascending;

@@ -70,7 +70,7 @@ _SIGNATURES = {
 _ATTENTION_SIGNATURES = {
     "sr_rope_kv_append": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _int, _f32, _vp, _vp, _i64, _vp, _i64, _vp]),
     "sr_kv_gather": (_int, [_vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp]),
-    "sr_attn_decode_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i64, _i64]),
+    "sr_attn_decode_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i64, _i64, _int]),
     "sr_attn_decode": (_int, [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _f32, _vp, _i64, _vp, _sz, _vp]),
     "sr_attn_prefill": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _int, _f32, _vp, _i64, _vp]),
 }
@@ -287,8 +287,9 @@ def sr_kv_gather(slots, cache, K_out=None, V_out=None):
     return out if type(out) is tuple else _refused(out, "sr_kv_gather")
 
 
-def sr_attn_decode_workspace_bytes(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, max_pages: int, page_size: int) -> int:
-    return int(raw().sr_attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim, max_pages, page_size))
+def sr_attn_decode_workspace_bytes(n_seqs: int, n_heads: int, n_kv_heads: int, head_dim: int, max_pages: int, page_size: int,
+                                   kv_type: int = SR_KV_I4) -> int:
+    return int(raw().sr_attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim, max_pages, page_size, kv_type))
 
 
 def sr_attn_decode(Q, cache, page_table, seq_lens, scale=None, O=None, workspace=None):

@@ -30,7 +30,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 union Frag { f16x8 v; uint32_t w[4]; _Float16 h[8]; };
 
 constexpr int kWaves = 4, kTile = 32, kRound = kWaves * kTile;
-constexpr int kLeast = 2;                                // rounds of a share, at least
 constexpr float kNone = -__builtin_inff();
 
 struct Decode {
@@ -71,7 +70,7 @@ __device__ __forceinline__ int share_size(const Decode &a, int lane)
     int sum = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) sum += rounds_of(a, b0 + lane);
     const int all = __builtin_amdgcn_readlane(scan_of_wave(sum), 63);
-    return max((all + a.shares - 1) / a.shares, kLeast);
+    return max((all + a.shares - 1) / a.shares, 1);
 }
 // rounds of the sequences before b
 __device__ __forceinline__ int rounds_before(const Decode &a, int b, int lane)
@@ -608,22 +607,28 @@ template <int D> hipError_t launch_join(const Decode &a, hipStream_t st)
 }
 
 // Shares of the sequences of one key/value head and row tile; 0: a workgroup per sequence does it all, which needs no second
-// kernel.
-int shares_of(int64_t n_seqs, int64_t per_seq, int64_t max_len)
+// kernel (4 us) and no change from one sequence to the next, but takes as long as the longest sequence: 0.8 us a round (4 bits;
+// fp16, which keeps one tile of a wave on its way, 1.6), or what the bytes take.  Measured (us, shares / a workgroup each):
+//   4 bits, 8 key/value heads of 128:  1 sequence of 500 tokens 8.7 / 7.2, 768 8.7 / 8.6, 1000 8.7 / 10.2;  8 of 500 9.3 / 7.5, 1000
+//     10.4 / 10.7;  16 of up to 1000 13.8 / 10.7, 2000 16.7 / 17.0;  32 of up to 2000 21.5 / 17.6, 3000 22.5 / 23.4;  64 of up to 2000
+//     26.6 / 23.0, 8192 56 / 95;  128 of up to 2000 45 / 37, 4096 60 / 67
+//   fp16:  1 of 384 8.7 / 7.2;  8 of 500 10.2 / 11.2;  32 of 500 17.4 / 13.5;  64 of up to 1000 30.5 / 33.5
+int shares_of(int64_t n_seqs, int64_t per_seq, int64_t max_len, bool i4)
 {
-    const int64_t want = (int64_t)compute_units() * 2;
-    const int64_t shares = want / per_seq;
-    if (shares < 2 || n_seqs > 1024 || n_seqs * per_seq >= 4 * want || max_len <= kLeast * kRound) return 0;
-    if (n_seqs * ((max_len + kRound - 1) / kRound) >= 1 << 30) return 0;     // rounds are counted in 32 bits
+    const int64_t units = compute_units(), rounds = (max_len + kRound - 1) / kRound, shares = 2 * units / per_seq;
+    const bool many = n_seqs * per_seq >= units / 2;
+    if (rounds <= (i4 ? (many ? 16 : 6) : (many ? 6 : 3))) return 0;
+    // a wave adds up 64 lengths at a time, and rounds are counted in 32 bits
+    if (shares < 2 || n_seqs > 1024 || n_seqs * per_seq >= 8 * units || n_seqs * rounds >= 1 << 30) return 0;
     return (int)shares;
 }
 
 }  // namespace
 
-size_t attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t kv, int64_t dim, int64_t max_len)
+size_t attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t kv, int64_t dim, int64_t max_len, bool i4)
 {
     const int64_t group = n_heads / kv, per_seq = kv * ((group + 15) / 16);
-    return (size_t)(per_seq * shares_of(n_seqs, per_seq, max_len) * 2 * (group < 16 ? group : 16) * (dim + 2) * 4);
+    return (size_t)(per_seq * shares_of(n_seqs, per_seq, max_len, i4) * 2 * (group < 16 ? group : 16) * (dim + 2) * 4);
 }
 
 hipError_t launch_attn_decode(const void *Q, int64_t ldq, int64_t n_seqs, int64_t n_heads, const KvCache &c, const int32_t *table,
@@ -637,7 +642,7 @@ hipError_t launch_attn_decode(const void *Q, int64_t ldq, int64_t n_seqs, int64_
     a.n_pages = (uint32_t)c.pages, a.page_shift = __builtin_ctzll((unsigned long long)c.page_size);
     a.table = table, a.ld_table = ld_table, a.max_len = max_pages * c.page_size, a.lens = lens;
     a.scale = scale * 1.4426950408889634f;
-    a.n_seqs = (int)n_seqs, a.per_seq = a.kv * a.row_tiles, a.shares = shares_of(n_seqs, a.per_seq, a.max_len);
+    a.n_seqs = (int)n_seqs, a.per_seq = a.kv * a.row_tiles, a.shares = shares_of(n_seqs, a.per_seq, a.max_len, c.i4);
     a.o = static_cast<_Float16 *>(O), a.ldo = ldo;
     a.part = static_cast<float *>(workspace);
     a.part_ml = a.part + (size_t)a.per_seq * a.shares * 2 * (a.group < 16 ? a.group : 16) * c.dim;

@@ -439,7 +439,7 @@ PyObject *attn_decode(PyObject *const *a)
     if (a[6] != Py_None) {
         work = here(tensor(a[6], "workspace"), "workspace");
         if (!work.is_contiguous()) value_error("%s must be contiguous", "workspace");
-    } else if (const size_t need = sr_attn_decode_workspace_bytes(B, heads, c.n_kv_heads, c.head_dim, pages, c.page_size)) {
+    } else if (const size_t need = sr_attn_decode_workspace_bytes(B, heads, c.n_kv_heads, c.head_dim, pages, c.page_size, c.type)) {
         work = empty({(int64_t)need}, at::kByte, Q);
     }
     const void *q = Q.data_ptr();

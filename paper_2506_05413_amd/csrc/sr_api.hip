@@ -383,10 +383,10 @@ static bool decode_shape_ok(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads,
 }
 
 size_t sr_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int64_t max_pages,
-                                      int64_t page_size)
+                                      int64_t page_size, int type)
 {
-    if (n_seqs <= 0 || !head_dim_ok(head_dim) || !decode_shape_ok(n_seqs, n_heads, n_kv_heads, max_pages, page_size)) return 0;
-    return sr::attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim, max_pages * page_size);
+    if ((type != SR_KV_F16 && type != SR_KV_I4) || n_seqs <= 0 || !head_dim_ok(head_dim) || !decode_shape_ok(n_seqs, n_heads, n_kv_heads, max_pages, page_size)) return 0;
+    return sr::attn_decode_workspace_bytes(n_seqs, n_heads, n_kv_heads, head_dim, max_pages * page_size, type == SR_KV_I4);
 }
 
 int sr_attn_decode(const void *Q_f16, int64_t ldq, int64_t n_seqs, int64_t n_heads, const sr_kv_cache *cache,
@@ -401,7 +401,7 @@ int sr_attn_decode(const void *Q_f16, int64_t ldq, int64_t n_seqs, int64_t n_hea
     if (n_seqs == 0) return SR_OK;
     if (!Q_f16 || !page_table || !seq_lens || !O_f16) return SR_ERR_NULL;
     if (ldq % 8 != 0 || ldo % 8 != 0 || !aligned16(Q_f16) || !aligned16(O_f16)) return SR_ERR_ALIGN;
-    const size_t need = sr::attn_decode_workspace_bytes(n_seqs, n_heads, c.heads, c.dim, max_pages * c.page_size);
+    const size_t need = sr::attn_decode_workspace_bytes(n_seqs, n_heads, c.heads, c.dim, max_pages * c.page_size, c.i4);
     if (need && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u))) return SR_ERR_WORKSPACE;
     return dev(sr::launch_attn_decode(Q_f16, ldq, n_seqs, n_heads, c, page_table, max_pages, ld_table, seq_lens, scale, O_f16, ldo,
                                       workspace, static_cast<hipStream_t>(stream)));

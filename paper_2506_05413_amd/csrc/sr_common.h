@@ -185,7 +185,7 @@ hipError_t launch_kv_gather(const int64_t *slots, int64_t T, const KvCache &c, v
                             hipStream_t st);
 
 // attention of one token per sequence over the cache (see attn_decode.hip); max_len = tokens that the page table covers
-size_t attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t kv, int64_t dim, int64_t max_len);
+size_t attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t kv, int64_t dim, int64_t max_len, bool i4);
 hipError_t launch_attn_decode(const void *Q, int64_t ldq, int64_t n_seqs, int64_t n_heads, const KvCache &c, const int32_t *table,
                               int64_t max_pages, int64_t ld_table, const int32_t *lens, float scale, void *O, int64_t ldo,
                               void *workspace, hipStream_t st);

@@ -121,7 +121,8 @@ def test_decode_workspace():
     assert decode(c, **wide, ws_bytes=need - 1) == sr.SR_ERR_WORKSPACE
     assert decode(c, **wide, ws=WS + 16) == sr.SR_ERR_WORKSPACE
     assert f(0, 32, 8, 128, 512, 64) == f(1, 32, 8, 96, 512, 64) == f(1, 30, 8, 128, 512, 64) == f(1, 32, 8, 128, 0, 64) == f(1, 32, 8, 128, 1 << 30, 64) == 0
-    assert f(1, 32, 8, 128, 1, 16) == 0
+    assert f(1, 32, 8, 128, 1, 16) == f(1, 32, 8, 128, 512, 64, 2) == f(1, 32, 8, 128, 512, 64, -1) == 0
+    assert f(1, 32, 8, 128, 512, 64, sr.SR_KV_F16) > 0
 
 
 @pytest.mark.parametrize("changed,status", [

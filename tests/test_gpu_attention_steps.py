@@ -95,19 +95,22 @@ def decode_step(s, x, pos, slots, table, lens, out, work):
     return gpu.sr_attn_prefill(Q, K, V, cu, cu, D)
 
 
-def grown(gpu, seed):
+def grown(gpu, seed, pages=20):
     s = Server(gpu, seed)
     x, pos, slots, _, _ = s.step((150, 290))
     s.append(x, pos, slots)
     x, pos, slots, _, _ = s.step((1, 1))
-    table = dev(s.pages)
+    table = torch.full((2, pages), -1, dtype=torch.int32, device="cuda")
+    table[:, :s.pages.shape[1]] = dev(s.pages)
     work = torch.zeros(max(1, gpu.sr_attn_decode_workspace_bytes(2, H, KV, D, table.shape[1], PAGE)), dtype=torch.uint8, device="cuda")
     return s, x, pos, slots, table, dev(np.array(s.lens(), np.int32)), torch.zeros((2, H * D), dtype=torch.float16, device="cuda"), work
 
 
-def test_two_streams_at_once(gpu):
+@pytest.mark.parametrize("pages", [20, 100])     # without shares of the sequences and with them
+def test_two_streams_at_once(gpu, pages):
     """Each stream its own cache, outputs and workspace: what one after the other gives, bit for bit."""
-    many = [grown(gpu, seed) for seed in (1, 2)]
+    many = [grown(gpu, seed, pages) for seed in (1, 2)]
+    assert (many[0][7].numel() > 1) == (pages == 100)
     want = []
     for m in many:
         p = decode_step(*m)
@@ -126,10 +129,11 @@ def test_two_streams_at_once(gpu):
             assert torch.equal(m[6], o) and torch.equal(p, q)
 
 
-def test_captured_step_replayed_on_new_inputs(gpu):
+@pytest.mark.parametrize("pages", [20, 100])
+def test_captured_step_replayed_on_new_inputs(gpu, pages):
     """A decode step captured once; inputs, lengths, positions and slots change between the replays, with eager work and other
     captures' workspace in between."""
-    s, x, pos, slots, table, lens, out, work = grown(gpu, 3)
+    s, x, pos, slots, table, lens, out, work = grown(gpu, 3, pages)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
@@ -152,8 +156,9 @@ def test_captured_step_replayed_on_new_inputs(gpu):
         assert torch.equal(got, eager_out) and torch.equal(p, want), i
 
 
-def test_same_call_same_bits(gpu):
-    m = grown(gpu, 4)
+@pytest.mark.parametrize("pages", [20, 100])
+def test_same_call_same_bits(gpu, pages):
+    m = grown(gpu, 4, pages)
     first = decode_step(*m).clone()
     o = m[6].clone()
     for _ in range(5):

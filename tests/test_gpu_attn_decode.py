@@ -101,9 +101,20 @@ def test_long_sequences_are_split_and_joined(gpu, i4, page):
     print("case decode long", page, i4, flush=True)
     for lens in ([5001], [3, 4097, 0, 2500]):
         batch = Batch(lens, 2, 128, page, i4, seed=page)
-        assert gpu.sr_attn_decode_workspace_bytes(len(lens), 8, 2, 128, batch.table.shape[1], page) > 0
+        assert gpu.sr_attn_decode_workspace_bytes(len(lens), 8, 2, 128, batch.table.shape[1], page, int(i4)) > 0
         q = queries(len(lens), 8, 128)
         batch.check(run(gpu, batch, q), q, 1 / np.sqrt(128))
+
+
+@pytest.mark.parametrize("i4", [True, False])
+@pytest.mark.parametrize("n,longest,shares", [(1, 380, False), (1, 800, True), (16, 760, False), (16, 2100, True)])
+def test_both_sides_of_the_choice(gpu, i4, n, longest, shares):
+    """One workgroup per sequence, and shares of them: few sequences and many."""
+    lens = [longest] + [int(x) for x in np.random.default_rng(n).integers(0, longest, n - 1)]
+    batch = Batch(lens, 8, 128, 16, i4, seed=n)
+    assert (gpu.sr_attn_decode_workspace_bytes(n, 16, 8, 128, batch.table.shape[1], 16, int(i4)) > 0) == shares
+    q = queries(n, 16, 128)
+    batch.check(run(gpu, batch, q), q, 1 / np.sqrt(128))
 
 
 @pytest.mark.parametrize("i4", [True, False])
