@@ -18,17 +18,19 @@
 // rescale nothing.  They are rounded to fp16 for the matrix pipe (half a step, 2^-11 of each; subnormal below 2^-21 of the largest
 // at least), and the sum in the denominator is that of the rounded ones.  Scores, sums and outputs are held in fp32.
 //
-// What bounds it: long prompts the power the chip may draw (8192 tokens, 32 heads of 128, causal, 128 rows a workgroup: the clock is
-// 1.83 GHz of 2.4 and the matrix pipe busy for half of the cycles; leaving out the exponentials, the reads from LDS or the DMA
-// loads in turn raised the clock and kept the count of cycles), short ones the chain of a row's tiles (1.3 us each with one wave
-// per SIMD).  Hence three shapes of workgroup (us for one prompt of T tokens, 32 heads and 8 key/value heads of 128, causal):
-//                                                                          T = 512   1024   2048   4096   8192
-//   8 row waves        a tile loaded once for 256 rows                        19.2   31.1   56.9    141    518
-//   4 row waves        128 rows, two workgroups on a compute unit             13.9   23.7   47.4    146    537
-//   2 row waves x 2    64 rows; two sets of waves take every other tile       11.6   24.3   65.1    209    772
-//                      and meet in LDS at the end
+// What bounds it: long prompts the power the chip may draw (8192 tokens, 32 heads of 128, causal: the clock is 1.83 GHz of 2.4 and
+// the matrix pipe busy for half of the cycles), the others the chain of a row's tiles.  Per 64 keys and SIMD, two waves there, the
+// products alone take 0.85 us, with the weights 1.05, with the reads from LDS 1.3; one wave takes 1.05.  Hence four shapes of
+// workgroup (us for one prompt of T tokens, 32 heads and 8 key/value heads of 128, causal; then 8 heads):
+//                                                            T = 512   1024   2048   4096   8192     2048   3000   4096
+//   8 row waves      a tile loaded once for 256 rows            19.2   31.1   56.9    141    518                     94
+//   4 row waves      128 rows, two workgroups on a unit         13.9   23.7   47.4    146    537              52     71
+//   2 x 2 sets       64 rows; the sets take every other         11.6   24.3   65.1    209    772     27.2     39     56
+//                    tile and meet in LDS at the end
+//   2 x 4 sets       tiles of 32 keys, two waves per SIMD       12.5   25.1                          25.5     34     53
 // Products interleaved with the weights of the tile before (three tiles in flight) were 9 % slower at 8192 tokens and 15 % at
-// 1024, 64 rows per wave (one wave per SIMD) 30 % slower.
+// 1024, 64 rows per wave (one wave per SIMD) 30 % slower, and two halves of a workgroup that multiply and weigh in turn, by
+// barriers, 6 .. 30 % slower.
 #include "gemm_common.h"
 
 namespace sr {
@@ -41,7 +43,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 union Frag { f16x8 v; s16x4 s[2]; f16x2 p[4]; };
 
-constexpr int kKeys = 64;                                // keys of a tile
 constexpr int kMatrix = 0x8, kRead = 0x100;              // groups of instructions for the scheduler: matrix products, reads from LDS
 constexpr float kNone = -__builtin_inff();
 
@@ -130,13 +131,13 @@ template <int ROWS> __device__ __forceinline__ bool find_tile(const Prefill &a, 
     return false;
 }
 
-// SETS sets of waves, each with every SETS-th tile of keys
-template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2) void attn_prefill_kernel(Prefill a)
+// SETS sets of waves, each with every SETS-th tile of KEYS keys
+template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W * SETS, D == 64 && SETS == 4 ? 4 : 2) void attn_prefill_kernel(Prefill a)
 {
     constexpr int ROWS = 32 * W;
     constexpr int CH = D / 8;                            // 16-byte chunks of a row
-    constexpr uint32_t kTileBytes = kKeys * D * 2;
-    constexpr int DT = D / 32, LOADS = kKeys * CH / (64 * W);    // column tiles; DMA loads of a wave per operand
+    constexpr uint32_t kTileBytes = KEYS * D * 2;
+    constexpr int DT = D / 32, LOADS = KEYS * CH / (64 * W);    // column tiles; DMA loads of a wave per operand
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];   // per set: [2][keys, values]
     const int lane = threadIdx.x & 63, m = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % W), set = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) / W);
@@ -170,7 +171,7 @@ template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2)
     auto load = [&](int t0, int slot) {
         const uint8_t *kt = kb + (int64_t)t0 * a.ldk * 2, *vt = vb + (int64_t)t0 * a.ldv * 2;
         const uint32_t to = lds + slot * 2 * kTileBytes + wave * 1024;
-        if (t0 + kKeys <= p.nk) {
+        if (t0 + KEYS <= p.nk) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 dma16(kt, k_off[i], to + W * 1024 * i);
@@ -186,9 +187,9 @@ template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2)
             }
         }
     };
-    const int n_tiles = end > 0 ? (end + kKeys - 1) / kKeys : 0, mine = wend > 0 ? (wend + kKeys - 1) / kKeys : 0;
+    const int n_tiles = end > 0 ? (end + KEYS - 1) / KEYS : 0, mine = wend > 0 ? (wend + KEYS - 1) / KEYS : 0;
     const int rounds = (n_tiles + SETS - 1) / SETS;
-    if (set < n_tiles) load(set * kKeys, 0);
+    if (set < n_tiles) load(set * KEYS, 0);
 
     Frag q[D / 16];
     {
@@ -209,12 +210,12 @@ template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2)
         wait_vmcnt<0>();
         barrier_nofence();
         const int next = (round + 1) * SETS + set;
-        if (next < n_tiles) load(next * kKeys, (round + 1) & 1);
+        if (next < n_tiles) load(next * KEYS, (round + 1) & 1);
     };
     int round = 0;
     for (; round * SETS + set < mine; ++round) {
         turn(round);
-        const int t0 = (round * SETS + set) * kKeys;
+        const int t0 = (round * SETS + set) * KEYS;
         const uint8_t *ks = tiles + (round & 1) * 2 * kTileBytes, *vs = ks + kTileBytes;
         auto value = [&](int step, int t) {
             Frag v;
@@ -227,9 +228,9 @@ template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2)
             }
             return v;
         };
-        f32x16 s[2];
+        f32x16 s[KEYS / 32];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < KEYS / 32; ++u) {
             s[u] = 0.f;
             const int r = 32 * u + m;
 #pragma unroll
@@ -239,27 +240,28 @@ template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2)
                 s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k.v, q[d].v, s[u], 0, 0, 0);
             }
         }
-        // six keys' reads ahead of the products, one more with each
-        __builtin_amdgcn_sched_group_barrier(kRead, 6, 0);
+        // reads of keys ahead of the products, one more with each
+        constexpr int SCORES = KEYS / 32 * (D / 16), AHEAD = SCORES > 8 ? 6 : SCORES / 2;
+        __builtin_amdgcn_sched_group_barrier(kRead, AHEAD, 0);
 #pragma unroll
-        for (int i = 0; i < D / 8 - 6; ++i) {
+        for (int i = 0; i < SCORES - AHEAD; ++i) {
             __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
             __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 6, 0);
-        if (t0 + kKeys > whole) {
+        __builtin_amdgcn_sched_group_barrier(kMatrix, AHEAD, 0);
+        if (t0 + KEYS > whole) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < KEYS / 32; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (t0 + 32 * u + 8 * (e / 4) + 4 * g + (e & 3) >= rend) s[u][e] = kNone;
         }
-        Frag w[4];                                       // of 16 tokens each
+        Frag w[KEYS / 16];                               // of 16 tokens each
         float sum;
         auto weigh = [&] {
             sum = 0.f;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < KEYS / 32; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
                     f16x2 &pair = w[2 * u + e / 8].p[e / 2 % 4];
@@ -271,7 +273,7 @@ template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2)
         if (!__all(sum <= limit)) {                      // (a weight beyond fp16 is infinite, and so is the sum)
             float most = kNone;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < KEYS / 32; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) most = fmaxf(most, s[u][e]);
             most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), top);
@@ -286,71 +288,81 @@ template <int D, int W, int SETS> __global__ __launch_bounds__(64 * W * SETS, 2)
         }
         total += sum;
 #pragma unroll
-        for (int step = 0; step < 4; ++step)
+        for (int step = 0; step < KEYS / 16; ++step)
 #pragma unroll
             for (int t = 0; t < DT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(step, t).v, w[step].v, acc[t], 0, 0, 0);
-        // eight reads (of four products) ahead, two more with each
-        __builtin_amdgcn_sched_group_barrier(kRead, 8, 1);
+        // the reads of some products ahead, two more with each
+        constexpr int VALUES = KEYS / 16 * DT, BEFORE = VALUES > 4 ? 4 : 2;
+        __builtin_amdgcn_sched_group_barrier(kRead, 2 * BEFORE, 1);
 #pragma unroll
-        for (int i = 0; i < 4 * DT - 4; ++i) {
+        for (int i = 0; i < VALUES - BEFORE; ++i) {
             __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 1);
             __builtin_amdgcn_sched_group_barrier(kRead, 2, 1);
         }
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 1);
+        __builtin_amdgcn_sched_group_barrier(kMatrix, BEFORE, 1);
     }
     for (; round < rounds; ++round) turn(round);         // tiles that only other waves need
 
-    if constexpr (SETS == 2) {
-        // the second set hands over what it has: 16 bytes of a lane beside those of the next
-        barrier_nofence();
-        f32x4 *area = reinterpret_cast<f32x4 *>(smem + wave * (D / 8 * 1024));
-        float2 *state = reinterpret_cast<float2 *>(smem + W * (D / 8 * 1024)) + wave * 64;
-        if (set == 1) {
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) area[(4 * t + e) * 64 + lane] = f32x4{acc[t][4 * e], acc[t][4 * e + 1], acc[t][4 * e + 2], acc[t][4 * e + 3]};
-            state[lane] = make_float2(top == kNone ? kNone : base, total);
-        }
-        __syncthreads();
-        if (set == 1) return;
-        const float2 other = state[lane];
-        const float own = top == kNone ? kNone : base, both = fmaxf(own, other.x);
-        const float mine_by = own == kNone ? 0.f : __builtin_amdgcn_exp2f(own - both), other_by = other.x == kNone ? 0.f : __builtin_amdgcn_exp2f(other.x - both);
-        total = total * mine_by + other.y * other_by;
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const f32x4 y = area[(4 * t + e) * 64 + lane];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[t][4 * e + r] = acc[t][4 * e + r] * mine_by + y[r] * other_by;
-            }
-    }
-    total += __shfl_xor(total, 32, 64);
-    if (row >= p.nq) return;
-    const float norm = total > 0.f ? 1.f / total : 0.f;
+    // a row's output is four neighbouring columns at a time: part i is those from 8 i + 4 g on
+    constexpr int PARTS = D / 8;
     _Float16 *dst = a.o + (int64_t)(p.q0 + row) * a.ldo + (int64_t)head * D + 4 * g;
+    auto store = [&](int i, f32x4 y) {
+        union { _Float16 h[4]; uint2 u; } v;
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+        for (int r = 0; r < 4; ++r) v.h[r] = (_Float16)y[r];
+        *reinterpret_cast<uint2 *>(dst + 8 * i) = v.u;
+    };
+    auto part = [&](int i) { return f32x4{acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2], acc[i / 4][4 * (i % 4) + 3]}; };
+    if constexpr (SETS == 1) {
+        total += __shfl_xor(total, 32, 64);
+        if (row >= p.nq) return;
+        const float norm = total > 0.f ? 1.f / total : 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            union { _Float16 h[4]; uint2 u; } y;
+        for (int i = 0; i < PARTS; ++i) store(i, part(i) * norm);
+    } else {
+        // the sets lay down what they have, 16 bytes of a lane beside those of the next, and each joins its share of the columns
+        barrier_nofence();
+        f32x4 *area = reinterpret_cast<f32x4 *>(smem) + wave * (PARTS * 64);
+        float2 *state = reinterpret_cast<float2 *>(smem + SETS * W * (PARTS * 1024)) + wave * 64;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y.h[r] = (_Float16)(acc[t][4 * e + r] * norm);
-            *reinterpret_cast<uint2 *>(dst + 32 * t + 8 * e) = y.u;
+        for (int i = 0; i < PARTS; ++i) area[(set * W * PARTS + i) * 64 + lane] = part(i);
+        state[set * W * 64 + lane] = make_float2(top == kNone ? kNone : base, total);
+        __syncthreads();
+        float by[SETS], both = kNone;
+#pragma unroll
+        for (int n = 0; n < SETS; ++n) both = fmaxf(both, state[n * W * 64 + lane].x);
+        total = 0.f;
+#pragma unroll
+        for (int n = 0; n < SETS; ++n) {
+            const float2 one = state[n * W * 64 + lane];
+            by[n] = one.x == kNone ? 0.f : __builtin_amdgcn_exp2f(one.x - both);
+            total += one.y * by[n];
         }
+        total += __shfl_xor(total, 32, 64);
+        if (row >= p.nq) return;
+        const float norm = total > 0.f ? 1.f / total : 0.f;
+#pragma unroll
+        for (int n = 0; n < SETS; ++n) by[n] *= norm;
+#pragma unroll
+        for (int j = 0; j < PARTS / SETS; ++j) {
+            const int i = set * (PARTS / SETS) + j;
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int n = 0; n < SETS; ++n) y += area[(n * W * PARTS + i) * 64 + lane] * by[n];
+            store(i, y);
+        }
+    }
 }
 
 // tiles of rows, at most: every sequence may end inside one
 int64_t tiles_of(int64_t T_q, int64_t n_seqs, int64_t rows) { return T_q / rows + (n_seqs < T_q ? n_seqs : T_q); }
 
-template <int D, int W, int SETS> hipError_t launch_dim(Prefill a, int64_t n_seqs, hipStream_t st)
+template <int D, int W, int SETS, int KEYS> hipError_t launch_dim(Prefill a, int64_t n_seqs, hipStream_t st)
 {
-    constexpr int bytes = SETS * 4 * kKeys * D * 2;
-    if (hipError_t e = allow_dynamic_lds<attn_prefill_kernel<D, W, SETS>>(bytes); e != hipSuccess) return e;
+    constexpr int tiles = SETS * 4 * KEYS * D * 2, join = SETS == 1 ? 0 : SETS * W * (D / 8 * 1024 + 512), bytes = tiles > join ? tiles : join;
+    if (hipError_t e = allow_dynamic_lds<attn_prefill_kernel<D, W, SETS, KEYS>>(bytes); e != hipSuccess) return e;
     a.tiles = (int)tiles_of(a.tokens_q, n_seqs, 32 * W);
-    hipLaunchKernelGGL((attn_prefill_kernel<D, W, SETS>), dim3((unsigned)((int64_t)a.tiles * a.heads)), dim3(64 * W * SETS), bytes, st, a);
+    hipLaunchKernelGGL((attn_prefill_kernel<D, W, SETS, KEYS>), dim3((unsigned)((int64_t)a.tiles * a.heads)), dim3(64 * W * SETS), bytes, st, a);
     return hipGetLastError();
 }
 
@@ -370,14 +382,18 @@ hipError_t launch_attn_prefill(const void *Q, int64_t ldq, const void *K, int64_
     a.heads = (int)n_heads, a.kv = (int)kv;
     a.causal = causal, a.scale = scale * 1.4426950408889634f;
     a.o = static_cast<_Float16 *>(O), a.ldo = ldo;
-    // Two sets of waves while the workgroups of 64 rows have their places at once; 256 rows where there are two rounds of such
-    // workgroups of long sequences (heads of 64 gain nothing: 4096 tokens, 32 heads 93 us for 91).
-    const int64_t units = compute_units();
+    // 64 rows while such workgroups have their places at once, and for long sequences while two rounds of them suffice: with four
+    // sets of waves from 2048 keys of a sequence on (heads of 64: 1024).  256 rows where two rounds of those workgroups are there
+    // (heads of 64 gain nothing: 4096 tokens, 32 heads 93 us for 91).
+    const int64_t units = compute_units(), places = units * (128 / dim), rows = T_q * n_heads;
     a.at_once = 0;
-    if (T_q * n_heads <= 64 * units * (128 / dim)) return dim == 128 ? launch_dim<128, 2, 2>(a, n_seqs, st) : launch_dim<64, 2, 2>(a, n_seqs, st);
-    if (dim == 128 && T_q * n_heads >= 2 * 256 * units && T_q >= 1024 * n_seqs) return launch_dim<128, 8, 1>(a, n_seqs, st);
+    if (rows <= 64 * places || (rows <= 144 * places && T_k > 1024 * n_seqs)) {
+        if (T_k * (128 / dim) >= 2048 * n_seqs) return dim == 128 ? launch_dim<128, 2, 4, 32>(a, n_seqs, st) : launch_dim<64, 2, 4, 32>(a, n_seqs, st);
+        return dim == 128 ? launch_dim<128, 2, 2, 64>(a, n_seqs, st) : launch_dim<64, 2, 2, 64>(a, n_seqs, st);
+    }
+    if (dim == 128 && rows >= 2 * 256 * units && T_q >= 1024 * n_seqs) return launch_dim<128, 8, 1, 64>(a, n_seqs, st);
     a.at_once = (int)((units + n_heads - 1) / n_heads);
-    return dim == 128 ? launch_dim<128, 4, 1>(a, n_seqs, st) : launch_dim<64, 4, 1>(a, n_seqs, st);
+    return dim == 128 ? launch_dim<128, 4, 1, 64>(a, n_seqs, st) : launch_dim<64, 4, 1, 64>(a, n_seqs, st);
 }
 
 }  // namespace sr
