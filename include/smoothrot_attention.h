@@ -26,7 +26,8 @@ enum { SR_KV_F16 = 0, SR_KV_I4 = 1 };
  * The cache: pages of page_size tokens, each page one head after the other.  Token i of a page is "slot" page * page_size + i.
  *   K, V                SR_KV_F16: fp16 [n_pages][n_kv_heads][page_size][head_dim]
  *                       SR_KV_I4:  uint8 [n_pages][n_kv_heads][page_size][head_dim / 2], packed like sr_kv_quant_asym's Q
- *   K_params, V_params  SR_KV_I4: fp32 [n_pages][n_kv_heads][page_size][2] (d, z): value = (code - z) * d.  NULL for SR_KV_F16.
+ *   K_params, V_params  SR_KV_I4: fp32 [n_pages][n_kv_heads][page_size][2] (d, z): value = (code - z) * d, d > 0, both finite.
+ *                       NULL for SR_KV_F16.
  * page_size a power of two, 16 <= page_size <= 2^20 (SR_ERR_ARG otherwise), n_pages >= 1, n_pages * page_size < 2^40.
  * The struct lies in host memory and is read during the call only.  Slots that no sequence holds may contain anything.
  */
@@ -85,7 +86,7 @@ SR_API int sr_kv_gather(const int64_t *slots, int64_t T, const sr_kv_cache *cach
  *                behind the length are not looked at; the tokens of an entry outside [0, n_pages) are left out.
  *   seq_lens     int32 [n_seqs], new token included; taken as 0 if negative and as max_pages * page_size if larger.
  *                A sequence without tokens gives zeros.
- *   scale        > 0 and finite
+ *   scale        0 < scale <= 2^64
  *   O_f16        out, fp16 [n_seqs, n_heads * head_dim], row stride ldo
  *   workspace    sr_attn_decode_workspace_bytes(...) bytes on the device that is current, 256-byte aligned (may be NULL where
  *                that is 0).  Contents need no initialisation; calls that share one must not overlap (captured graphs included).
@@ -109,7 +110,7 @@ SR_API int sr_attn_decode(const void *Q_f16, int64_t ldq, int64_t n_seqs, int64_
  *   K_f16, V_f16   fp16 [T_k, n_kv_heads * head_dim], row strides ldk, ldv (may be NULL with T_k = 0)
  *   cu_q, cu_k     int32 [n_seqs + 1]: sequence s holds rows cu_q[s] .. cu_q[s + 1] - 1 of Q and cu_k[s] .. of K and V (ascending;
  *                  cut to [0, T_q] and [0, T_k]).  Rows of no sequence are left as they were.
- *   scale          > 0 and finite
+ *   scale          0 < scale <= 2^64
  *   O_f16          out, fp16 [T_q, n_heads * head_dim], row stride ldo
  * T_q, T_k < 2^31, row strides < 2^23, (T_q / 64 + n_seqs) * n_heads < 2^31.  A non-finite key or value reaches rows of its own
  * sequence only.

@@ -2,7 +2,9 @@
 //
 //   s_t = scale q . k_t,   o = sum_t softmax(s)_t v_t     over the tokens t < length whose page exists
 //
-// Bound by the bytes of the cache.  A workgroup takes one key/value head (up to 16 of the query heads that share it) and runs of
+// Bound by the bytes of the cache where it is long (4 bits, 8 key/value heads of 128: 64 sequences of 0 .. 8192 tokens, 294 MB, in
+// 55 us = 5.3 TB/s; fp16, 32 heads of 64: 24 sequences of 2000 tokens, 241 MB, in 45 us), else by the launch and the chain of
+// loads of one sequence (130 tokens 5 us, 65000 tokens, 75 MB, 20 us with the join).  A workgroup takes one key/value head (up to 16 of the query heads that share it) and runs of
 // tokens; its four waves walk over tiles of 32 tokens with a running maximum and sum, and meet in LDS.  Both products run on
 // 16 x 16 x 32 matrix instructions with the query head in the columns:
 //
@@ -16,8 +18,9 @@
 // as exact as over c itself, to 2^-22, while over c 2^-24, bits 0-3, they are off by 2^-14 of a code.)  With scale d and zero z
 // per token,
 //   s_t = d (q . c - z sum(q)),   o = sum_t w_t (c_t - z_t),   w_t = p_t d_t
-// where the maximum that is kept is that of s log2(e) + log2(d): weights w then are at most 2^8 however large or small the
-// values are, and lose nothing to the range of fp16.  w is rounded to fp16 for the matrix pipe (half a step, 2^-11 of it; the
+// where p = 2^(s log2(e) - top - lift), top the maximum of the scores and lift that of the tokens' (score - top) + log2(d): weights
+// w then are at most 2^8 however large or small the values are, and lose nothing to the range of fp16.  (One sum of the two would
+// not do: beside a score of 2^28 it has no room for the other.)  w is rounded to fp16 for the matrix pipe (half a step, 2^-11 of it; the
 // same rounded w multiplies z), sums and maxima are fp32.
 #include "gemm_common.h"
 
@@ -30,7 +33,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 union Frag { f16x8 v; uint32_t w[4]; _Float16 h[8]; };
 
 constexpr int kWaves = 4, kTile = 32, kRound = kWaves * kTile;
-constexpr float kNone = -__builtin_inff();
+constexpr float kNone = -__builtin_inff(), kLeastLift = -40.f;
 
 struct Decode {
     const _Float16 *q;
@@ -147,7 +150,7 @@ template <int D, bool I4> struct Rows {
     Frag q[D / 32];
     float unit, qz;                                      // score of one product; its sum(q)
     f32x4 acc[C];                                        // sums of w c 2^-20, or w v
-    float top, total, zsum;                              // maximum; sums of p and w z over this lane's tokens
+    float top, lift, total, zsum;                        // maximum; sums of p and w z over this lane's tokens
 
     // row n of q, in the order that the keys lie in; zeros for a row that is not there
     __device__ __forceinline__ void begin(const _Float16 *src, bool there, int g, float scale)
@@ -173,13 +176,14 @@ template <int D, bool I4> struct Rows {
         unit = I4 ? scale * 1048576.f : scale, qz = qsum * scale;
 #pragma unroll
         for (int j = 0; j < C; ++j) acc[j] = 0.f;
-        top = kNone, total = 0.f, zsum = 0.f;
+        top = kNone, lift = 0.f, total = 0.f, zsum = 0.f;
     }
 
     // 32 tokens from `at` on, those before `last` whose page is there (bit u: of half u)
     __device__ __forceinline__ void use(T &t, int at, int last, uint32_t pages_there, int n, int g)
     {
-        float y[2][4];                                   // scores over log(2); for 4 bits still without the key's scale
+#pragma clang fp contract(off)                            // a score minus the maximum of the rounded ones is exact near it
+        float y[2][4];                                   // scores over log(2)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f32x4 dot = 0.f;
@@ -191,7 +195,7 @@ template <int D, bool I4> struct Rows {
                 dot = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.v, q[i].v, dot, 0, 0, 0);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[u][r] = I4 ? fmaf(dot[r], unit, -t.kz[u][r] * qz) : dot[r] * unit;
+            for (int r = 0; r < 4; ++r) y[u][r] = I4 ? fmaf(dot[r], unit, -t.kz[u][r] * qz) * t.ks[u][r] : dot[r] * unit;
         }
         if (pages_there != 3 || at + kTile > last) {     // a token that is not there: score minus infinity, a finite value
 #pragma unroll
@@ -201,7 +205,6 @@ template <int D, bool I4> struct Rows {
                     const bool there = (pages_there >> u & 1) && at + 16 * u + 4 * g + r < last;
                     y[u][r] = there ? y[u][r] : kNone;
                     if constexpr (I4) {
-                        t.ks[u][r] = there ? t.ks[u][r] : 1.f;
                         t.vs[u][r] = there ? t.vs[u][r] : 1.f;
                         t.vz[u][r] = there ? t.vz[u][r] : 0.f;
                     } else {
@@ -217,7 +220,7 @@ template <int D, bool I4> struct Rows {
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    p[u][r] = __builtin_amdgcn_exp2f(I4 ? fmaf(t.ks[u][r], y[u][r], -top) : y[u][r] - top);
+                    p[u][r] = __builtin_amdgcn_exp2f(I4 ? y[u][r] - top - lift : y[u][r] - top);
                     w[u][r] = I4 ? p[u][r] * t.vs[u][r] : p[u][r];
                     most = fmaxf(most, w[u][r]);
                 }
@@ -226,14 +229,23 @@ template <int D, bool I4> struct Rows {
         // Weights stay below 2^8 relative to a maximum that is replaced only when one does not (the first tile's always): fp16
         // has room for that, and most tiles then rescale nothing.
         if (!__all(weights() <= 256.f && top != kNone)) {
-            float most = kNone;
+            float most = kNone, raised = kLeastLift;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    most = fmaxf(most, I4 ? fmaf(t.ks[u][r], y[u][r], __builtin_amdgcn_logf(t.vs[u][r])) : y[u][r]);
+                for (int r = 0; r < 4; ++r) most = fmaxf(most, y[u][r]);
             most = fmaxf(top, max_of_groups(most));
-            const float shrink = most == kNone ? 1.f : __builtin_amdgcn_exp2f(top - most);
+            if constexpr (I4) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (most != kNone) raised = fmaxf(raised, y[u][r] - most + __builtin_amdgcn_logf(t.vs[u][r]));
+                raised = max_of_groups(raised);
+                if (top != kNone) raised = fmaxf(raised, top - most + lift);
+            }
+            const float shrink = most == kNone ? 1.f : __builtin_amdgcn_exp2f(I4 ? top - most + (lift - raised) : top - most);
+            if (I4 && most != kNone) lift = raised;
             total *= shrink;
             zsum *= shrink;
 #pragma unroll
@@ -465,7 +477,7 @@ template <int D, bool I4> __global__ __launch_bounds__(kWaves * 64, 2) void attn
         // the four waves meet: acc[j][r] of lane (n, g) is column d = C (4 g + r) + j of query row n
         float(*s_top)[16] = reinterpret_cast<float(*)[16]>(smem), (*s_total)[16] = s_top + kWaves;
         float(*s_acc)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(s_total + kWaves);
-        const float total = sum_of_groups(rows.total), zsum = sum_of_groups(rows.zsum);
+        const float back = I4 ? __builtin_amdgcn_exp2f(rows.lift) : 1.f, total = sum_of_groups(rows.total) * back, zsum = sum_of_groups(rows.zsum);
         if (g == 0) s_top[wave][n] = rows.top, s_total[wave][n] = total;
         if (n < n_rows) {
 #pragma unroll
@@ -474,7 +486,7 @@ template <int D, bool I4> __global__ __launch_bounds__(kWaves * 64, 2) void attn
                 for (int j = 0; j < C; j += 4) {
                     f32x4 x;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = I4 ? rows.acc[j + e][r] * 1048576.f - zsum : rows.acc[j + e][r];
+                    for (int e = 0; e < 4; ++e) x[e] = I4 ? (rows.acc[j + e][r] * 1048576.f - zsum) * back : rows.acc[j + e][r];
                     *reinterpret_cast<f32x4 *>(&s_acc[wave][n][C * (4 * g + r) + j]) = x;
                 }
         }

@@ -13,10 +13,11 @@
 // so weights stay in the lane that computed them, a row's sum is one lane's and its neighbour 32 further, and values are read
 // from LDS with the transposing 8-byte read (four tokens of one column per lane).
 //
-// Weights are w = exp2(score - base), a row's largest 2^7 when its base is set, and the base is set again only where one might
-// pass 2^16: the sum of a tile's weights, which is needed anyhow, shows it, so that a tile needs no maximum, and most tiles
-// rescale nothing.  They are rounded to fp16 for the matrix pipe (half a step, 2^-11 of each; subnormal below 2^-21 of the largest
-// at least), and the sum in the denominator is that of the rounded ones.  Scores, sums and outputs are held in fp32.
+// Weights are w = 2^(7 + log2(e) scale (q . k - top)), top a row's largest q . k when it was set, and it is set again only where a
+// weight might pass 2^16: the sum of a tile's weights, which is needed anyhow, shows it, so that a tile needs no maximum, and most
+// tiles rescale nothing.  The products of a tile are summed up from -top on, so that a difference is rounded as the score is,
+// however large.  Weights are rounded to fp16 for the matrix pipe (half a step, 2^-11 of each; subnormal below 2^-21 of the
+// largest at least), and the sum in the denominator is that of the rounded ones.  Scores, sums and outputs are held in fp32.
 //
 // What bounds it: long prompts the power the chip may draw (8192 tokens, 32 heads of 128, causal: the clock is 1.83 GHz of 2.4 and
 // the matrix pipe busy for half of the cycles), the others the chain of a row's tiles.  Per 64 keys and SIMD, two waves there, the
@@ -76,8 +77,8 @@ __device__ __forceinline__ void take(Place &p, int lane_of, int q0, int nq, int 
 }
 
 // The tile-th tile of rows of the batch, those with the most keys first; false behind the last.  A lane looks at a sequence.
-// (Nine prompts of 26 .. 541 tokens: 29.3 -> 25.7 us.)  Up to 64 sequences: tile i of a sequence that has `ahead` more keys than queries is on level i + 1 + ahead / ROWS, and a level
-// is found by bisection over the number of tiles above it.  Where every workgroup has its place at once (`at_once` tiles are
+// (Nine prompts of 26 .. 541 tokens: 29.3 -> 25.7 us.)  Up to 64 sequences: tile i of a sequence that has `ahead` more keys than
+// queries is on level i + 1 + ahead / ROWS, and a level is found by bisection over the number of tiles above it.  Where every workgroup has its place at once (`at_once` tiles are
 // half of the places), the second half of them is dealt out from the other end, so that a compute unit's two workgroups are a
 // long and a short one (one prompt of 2048 tokens, 32 heads of 128: 48.6 -> 47.4 us).  More sequences: the last one's last first.
 template <int ROWS> __device__ __forceinline__ bool find_tile(const Prefill &a, int tile, int lane, Place &p)
@@ -203,7 +204,8 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
     f32x16 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = 0.f;
-    float top = kNone, base = 0.f, limit = -1.f, total = 0.f;
+    f32x16 below = 0.f;                                  // minus the score that weights are relative to
+    float top = kNone, limit = -1.f, total = 0.f;
 
     // what was asked for a round ago is there, and everybody is done with the slot that is asked for now
     auto turn = [&](int round) {
@@ -231,7 +233,7 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
         f32x16 s[KEYS / 32];
 #pragma unroll
         for (int u = 0; u < KEYS / 32; ++u) {
-            s[u] = 0.f;
+            s[u] = below;
             const int r = 32 * u + m;
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
@@ -265,7 +267,7 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
                     f16x2 &pair = w[2 * u + e / 8].p[e / 2 % 4];
-                    pair = f16x2{(_Float16)__builtin_amdgcn_exp2f(fmaf(s[u][e], a.scale, -base)), (_Float16)__builtin_amdgcn_exp2f(fmaf(s[u][e + 1], a.scale, -base))};
+                    pair = f16x2{(_Float16)__builtin_amdgcn_exp2f(fmaf(s[u][e], a.scale, 7.f)), (_Float16)__builtin_amdgcn_exp2f(fmaf(s[u][e + 1], a.scale, 7.f))};
                     sum = __builtin_amdgcn_fdot2(pair, f16x2{(_Float16)1.f, (_Float16)1.f}, sum, false);
                 }
         };
@@ -276,13 +278,16 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
             for (int u = 0; u < KEYS / 32; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) most = fmaxf(most, s[u][e]);
-            most = fmaxf(fmaxf(most, __shfl_xor(most, 32, 64)), top);
-            if (most != kNone) {
-                const float now = most * a.scale - 7.f, shrink = top == kNone ? 1.f : __builtin_amdgcn_exp2f(base - now);
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            const float up = top == kNone ? most : fmaxf(most, 0.f);
+            if (up != kNone) {
+                const float shrink = top == kNone ? 1.f : __builtin_amdgcn_exp2f(-up * a.scale);
                 total *= shrink;
 #pragma unroll
                 for (int t = 0; t < DT; ++t) acc[t] *= shrink;
-                base = now, top = most, limit = 32768.f;
+#pragma unroll
+                for (int u = 0; u < KEYS / 32; ++u) s[u] -= up;
+                below -= up, top = -below[0], limit = 32768.f;
             }
             weigh();
         }
@@ -326,7 +331,7 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
         float2 *state = reinterpret_cast<float2 *>(smem + SETS * W * (PARTS * 1024)) + wave * 64;
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) area[(set * W * PARTS + i) * 64 + lane] = part(i);
-        state[set * W * 64 + lane] = make_float2(top == kNone ? kNone : base, total);
+        state[set * W * 64 + lane] = make_float2(top, total);
         __syncthreads();
         float by[SETS], both = kNone;
 #pragma unroll
@@ -335,7 +340,7 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
 #pragma unroll
         for (int n = 0; n < SETS; ++n) {
             const float2 one = state[n * W * 64 + lane];
-            by[n] = one.x == kNone ? 0.f : __builtin_amdgcn_exp2f(one.x - both);
+            by[n] = one.x == kNone ? 0.f : __builtin_amdgcn_exp2f((one.x - both) * a.scale);
             total += one.y * by[n];
         }
         total += __shfl_xor(total, 32, 64);

@@ -4,13 +4,13 @@
 //   Hadamard: y <- y H_D / sqrt(D) inside the head, butterflies over strides 1, 2, 4, ..
 //   4 bits, per token and head:  D = (hi - lo) * (1 / 15), z = -rint(lo / D), code = clamp(rint(v / D) + z, 0, 15)
 //
-// Every product, sum and quotient is rounded on its own (no fused multiply-add): keys are rounded to fp16 and values next to
-// a rounding boundary take the code that the formula in fp32 gives, whoever evaluates it.
+// Every product, sum and quotient comes out as rounded on its own: keys are rounded to fp16 and values next to a rounding
+// boundary take the code that the formula in fp32 gives, whoever evaluates it.
 //
 // Bound by its bytes where there are many tokens (16384 with 32 query heads and 8 key/value heads of 128, 4 bits: 363 MB in 80 us,
-// 4.5 TB/s; 2047 with the transform 14 us, 3.3 TB/s), else by the launch (one token 2.5 us).  Eight values (16 bytes) per lane, D / 8 lanes per row, a row being one head of one token, query, key or
-// value; the head's other half, the butterflies and the range of a row are exchanged between those lanes with operand
-// permutations, without LDS.
+// 4.5 TB/s; 2047 with the transform 14 us, 3.3 TB/s), else by the launch (one token 2.5 us).  Eight values (16 bytes) per lane,
+// D / 8 lanes per row, a row being one head of one token, query, key or value; the head's other half, the butterflies and the
+// range of a row are exchanged between those lanes with operand permutations, without LDS.
 #include "sr_common.h"
 
 namespace sr {

@@ -338,7 +338,7 @@ static bool heads_fit(int64_t n_heads, int64_t n_kv_heads)
 {
     return n_kv_heads >= 1 && n_heads >= n_kv_heads && n_heads < (1 << 20) && n_heads % n_kv_heads == 0;
 }
-static bool scale_ok(float scale) { return scale > 0.f && scale <= 3.4e38f; }
+static bool scale_ok(float scale) { return scale > 0.f && scale <= 0x1p64f; }            // scores stay finite
 
 int sr_rope_kv_append(const void *Q_f16, int64_t ldq, const void *K_f16, int64_t ldk, const void *V_f16, int64_t ldv,
                       int64_t T, int64_t n_heads, const int32_t *positions, const int64_t *slots,

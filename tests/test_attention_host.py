@@ -104,7 +104,7 @@ def test_gather_refusals(changed, status):
 @pytest.mark.parametrize("changed,status", [
     (dict(B=-1), sr.SR_ERR_SHAPE), (dict(B=1 << 20), sr.SR_ERR_SHAPE), (dict(H=0), sr.SR_ERR_SHAPE), (dict(H=7), sr.SR_ERR_SHAPE), (dict(H=1), sr.SR_ERR_SHAPE),
     (dict(pages=0), sr.SR_ERR_SHAPE), (dict(pages=(1 << 26) + 1, ld_table=1 << 27), sr.SR_ERR_SHAPE), (dict(ld_table=3), sr.SR_ERR_SHAPE), (dict(ldq=1016), sr.SR_ERR_SHAPE),
-    (dict(ldo=1016), sr.SR_ERR_SHAPE), (dict(scale=0.0), sr.SR_ERR_ARG), (dict(scale=-1.0), sr.SR_ERR_ARG), (dict(scale=NAN), sr.SR_ERR_ARG), (dict(scale=INF), sr.SR_ERR_ARG),
+    (dict(ldo=1016), sr.SR_ERR_SHAPE), (dict(scale=0.0), sr.SR_ERR_ARG), (dict(scale=-1.0), sr.SR_ERR_ARG), (dict(scale=NAN), sr.SR_ERR_ARG), (dict(scale=INF), sr.SR_ERR_ARG), (dict(scale=2e19), sr.SR_ERR_ARG),
     (dict(Q=None), sr.SR_ERR_NULL), (dict(table=None), sr.SR_ERR_NULL), (dict(lens=None), sr.SR_ERR_NULL), (dict(O=None), sr.SR_ERR_NULL),
     (dict(ldq=1028), sr.SR_ERR_ALIGN), (dict(ldo=1028), sr.SR_ERR_ALIGN), (dict(Q=A + 8), sr.SR_ERR_ALIGN), (dict(O=A + 8), sr.SR_ERR_ALIGN),
     (dict(B=0, Q=None, table=None, lens=None, O=None, ws=None, ws_bytes=0), sr.SR_OK)])
@@ -126,7 +126,7 @@ def test_decode_workspace():
 
 
 @pytest.mark.parametrize("changed,status", [
-    (dict(d=96), sr.SR_ERR_ARG), (dict(d=0), sr.SR_ERR_ARG), (dict(scale=0.0), sr.SR_ERR_ARG), (dict(scale=-0.5), sr.SR_ERR_ARG), (dict(scale=NAN), sr.SR_ERR_ARG), (dict(scale=INF), sr.SR_ERR_ARG),
+    (dict(d=96), sr.SR_ERR_ARG), (dict(d=0), sr.SR_ERR_ARG), (dict(scale=0.0), sr.SR_ERR_ARG), (dict(scale=-0.5), sr.SR_ERR_ARG), (dict(scale=NAN), sr.SR_ERR_ARG), (dict(scale=INF), sr.SR_ERR_ARG), (dict(scale=2e19), sr.SR_ERR_ARG),
     (dict(n=-1), sr.SR_ERR_SHAPE), (dict(Tq=-1), sr.SR_ERR_SHAPE), (dict(Tk=-1), sr.SR_ERR_SHAPE), (dict(Tq=1 << 31), sr.SR_ERR_SHAPE), (dict(Tk=1 << 31), sr.SR_ERR_SHAPE),
     (dict(H=0), sr.SR_ERR_SHAPE), (dict(H=7), sr.SR_ERR_SHAPE), (dict(KV=0), sr.SR_ERR_SHAPE), (dict(KV=16), sr.SR_ERR_SHAPE),
     (dict(ldq=1016), sr.SR_ERR_SHAPE), (dict(ldo=1016), sr.SR_ERR_SHAPE), (dict(ldk=248), sr.SR_ERR_SHAPE), (dict(ldv=248), sr.SR_ERR_SHAPE),

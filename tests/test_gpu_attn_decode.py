@@ -159,6 +159,35 @@ def test_small_large_and_shifted_values(gpu, i4, spread, offset):
 
 
 @pytest.mark.parametrize("i4", [True, False])
+@pytest.mark.parametrize("d", [128, 64])
+def test_scores_beyond_the_steps_of_fp32(gpu, i4, d):
+    """Scores up to 2^39, whose neighbouring fp32 numbers are 2^16 apart, every two of them further than that: all weight is on
+    the largest.  Off by the weight's and the output's rounding (2^-11 each) and those of the fp32 sums (2^-20 of their terms)."""
+    rng = np.random.default_rng(d)
+    lens = [300, 1, 1500]
+    batch = Batch(lens, 2, d, 16, i4, seed=d, spread=0.01)
+    q = np.full((3, 4, d), 30000, np.float16)
+    K, V, Kp, Vp = (None if t is None else t.cpu() for t in batch.cache)
+    best = np.zeros((3, 2), int)
+    for b, n in enumerate(lens):
+        for h in range(2):
+            size = rng.permutation(np.arange(500, 500 + n)).astype(np.float32)
+            best[b, h] = size.argmax()
+            for t in range(n):
+                page, at = batch.table[b, t // 16], t % 16
+                if i4:
+                    K[page, h, at], Kp[page, h, at] = 0x11, torch.tensor([float(size[t]), 0.0])
+                else:
+                    K[page, h, at] = float(size[t])
+    batch.cache = tuple(None if t is None else t.cuda() for t in (K, V, Kp, Vp))
+    got = run(gpu, batch, q, 64.0).astype(np.float64)
+    for b in range(3):
+        for head in range(4):
+            v, size = batch.v[b][best[b, head // 2], head // 2], batch.v_size[b][best[b, head // 2], head // 2]
+            assert (np.abs(got[b, head] - v) <= 2.0 ** -10 * np.abs(v) + 2.0 ** -20 * size + 2.0 ** -25).all(), (b, head)
+
+
+@pytest.mark.parametrize("i4", [True, False])
 @pytest.mark.parametrize("scale", [1e-4, 0.5, 3.0])
 def test_scales_from_flat_to_one_token(gpu, i4, scale):
     batch = Batch([300, 16], 1, 64, 16, i4)

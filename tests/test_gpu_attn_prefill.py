@@ -102,6 +102,24 @@ def test_scales_from_flat_to_one_token(gpu, scale):
     check(run(gpu, q, k, v, [150, 90], [150, 90], scale=scale), q, k, v, [150, 90], [150, 90], True, float(np.float32(scale)))
 
 
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("H,T", [(2, 300), (2, 1500), (26, 2048), (48, 1024)])
+def test_scores_beyond_the_steps_of_fp32(gpu, d, H, T):
+    """Scores up to 2^39, whose neighbouring fp32 numbers are 2^16 apart, every two of them further than that: all weight is on
+    the largest so far, a power of two that comes out again."""
+    q, k, v = make([T], [T], H, 1, d, seed=T)
+    size = np.random.default_rng(d).permutation(np.arange(T) % 1500 + 500 + np.arange(T) // 1500 * 0.5).astype(np.float16)
+    size = np.unique(size)                               # (fp16 holds the halves up to 1023.5)
+    T = len(size)
+    q, v = q[:T], v[:T]
+    np.random.default_rng(d).shuffle(size)
+    q[:], k = 30000, np.broadcast_to(size[:, None, None], (T, 1, d)).copy()
+    best = np.array([size[:i + 1].argmax() for i in range(T)])
+    got = run(gpu, q, k, v, [T], [T], True, 64.0)
+    for h in range(H):
+        np.testing.assert_array_equal(got[:, h], v[best, 0])
+
+
 def test_scores_that_grow_and_fall_along_the_keys(gpu):
     """The running maximum is replaced at every tile, and never."""
     T, d = 400, 128
