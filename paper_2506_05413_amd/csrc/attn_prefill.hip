@@ -190,14 +190,29 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
     };
     const int n_tiles = end > 0 ? (end + KEYS - 1) / KEYS : 0, mine = wend > 0 ? (wend + KEYS - 1) / KEYS : 0;
     const int rounds = (n_tiles + SETS - 1) / SETS;
-    if (set < n_tiles) load(set * KEYS, 0);
-
-    Frag q[D / 16];
+    // A wave's query rows come the same way, whole rows at a time, through the stage of the second tile (and past it: 8 row waves).
+    // Taken from memory in the order of the operand, every line of a row would be asked for four times.
+    constexpr int Q_LOADS = CH / 2;
+    constexpr uint32_t kQueries = 2 * kTileBytes;
     {
-        const _Float16 *src = a.q + (int64_t)(p.q0 + min(row, p.nq - 1)) * a.ldq + (int64_t)head * D + 8 * g;
+        const int b0 = min(w0, p.nq - 1);
+        const uint8_t *from = reinterpret_cast<const uint8_t *>(a.q + (int64_t)(p.q0 + b0) * a.ldq + (int64_t)head * D);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) q[i].v = *reinterpret_cast<const f16x8 *>(src + 16 * i);
+        for (int i = 0; i < Q_LOADS; ++i) {
+            const int at = i * 64 + lane, r = at / CH, c = at % CH;
+            dma16(from, (uint32_t)min(r, p.nq - 1 - b0) * (uint32_t)(a.ldq * 2) + 16 * (c ^ key_swap(r)), lds + kQueries + wave * (32 * D * 2) + 1024 * i);
+        }
     }
+    Frag q[D / 16];
+    if (set < n_tiles) {
+        load(set * KEYS, 0);
+        wait_vmcnt<2 * LOADS>();
+    } else {
+        wait_vmcnt<0>();
+    }
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+        q[i].v = *reinterpret_cast<const f16x8 *>(tiles + kQueries + wave * (32 * D * 2) + m * (D * 2) + 16 * ((2 * i + g) ^ key_swap(m)));
     // have them here: a wait for them inside the loop below would be one for everything that is in flight there
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(q[i].v));
@@ -308,53 +323,65 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
     }
     for (; round < rounds; ++round) turn(round);         // tiles that only other waves need
 
-    // a row's output is four neighbouring columns at a time: part i is those from 8 i + 4 g on
+    // Outputs leave as they came, whole rows at a time: a lane has four columns of a row (part i: those from 8 i + 4 g on) and
+    // stores eight of another one.
     constexpr int PARTS = D / 8;
-    _Float16 *dst = a.o + (int64_t)(p.q0 + row) * a.ldo + (int64_t)head * D + 4 * g;
-    auto store = [&](int i, f32x4 y) {
-        union { _Float16 h[4]; uint2 u; } v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v.h[r] = (_Float16)y[r];
-        *reinterpret_cast<uint2 *>(dst + 8 * i) = v.u;
-    };
     auto part = [&](int i) { return f32x4{acc[i / 4][4 * (i % 4)], acc[i / 4][4 * (i % 4) + 1], acc[i / 4][4 * (i % 4) + 2], acc[i / 4][4 * (i % 4) + 3]}; };
+    auto store = [&](int r, int c, f16x8 y) {
+        if (w0 + r < p.nq) *reinterpret_cast<f16x8 *>(a.o + (int64_t)(p.q0 + w0 + r) * a.ldo + (int64_t)head * D + 8 * c) = y;
+    };
+    barrier_nofence();
     if constexpr (SETS == 1) {
         total += __shfl_xor(total, 32, 64);
-        if (row >= p.nq) return;
         const float norm = total > 0.f ? 1.f / total : 0.f;
+        // chunks swapped by row, their halves by rows 16 and up
+        uint8_t *area = smem + wave * (32 * D * 2);
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) store(i, part(i) * norm);
+        for (int i = 0; i < PARTS; ++i) {
+            union { _Float16 h[4]; uint2 u; } y;
+            const f32x4 x = part(i) * norm;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y.h[e] = (_Float16)x[e];
+            *reinterpret_cast<uint2 *>(area + m * (D * 2) + 16 * (i ^ (m & (CH - 1))) + 8 * (g ^ (m >> 4))) = y.u;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < CH / 2; ++j) {
+            const int r = (j * 64 + lane) / CH, c = lane % CH;
+            f16x8 y = *reinterpret_cast<const f16x8 *>(area + r * (D * 2) + 16 * (c ^ (r & (CH - 1))));
+            if (j >= CH / 4) y = __builtin_shufflevector(y, y, 4, 5, 6, 7, 0, 1, 2, 3);
+            store(r, c, y);
+        }
     } else {
-        // the sets lay down what they have, 16 bytes of a lane beside those of the next, and each joins its share of the columns
-        barrier_nofence();
+        // the sets lay down what they have (part i of a lane beside those of others, in an order of its own), and each joins its
+        // share of the rows
         f32x4 *area = reinterpret_cast<f32x4 *>(smem) + wave * (PARTS * 64);
         float2 *state = reinterpret_cast<float2 *>(smem + SETS * W * (PARTS * 1024)) + wave * 64;
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) area[(set * W * PARTS + i) * 64 + lane] = part(i);
+        for (int i = 0; i < PARTS; ++i) area[(set * W * PARTS + i) * 64 + (lane ^ i)] = part(i);
         state[set * W * 64 + lane] = make_float2(top, total);
         __syncthreads();
-        float by[SETS], both = kNone;
 #pragma unroll
-        for (int n = 0; n < SETS; ++n) both = fmaxf(both, state[n * W * 64 + lane].x);
-        total = 0.f;
+        for (int j = 0; j < CH / 2 / SETS; ++j) {
+            const int r = ((set * (CH / 2 / SETS) + j) * 64 + lane) / CH, c = lane % CH;
+            float both = kNone, all = 0.f;
+            f32x4 lo = 0.f, hi = 0.f;
 #pragma unroll
-        for (int n = 0; n < SETS; ++n) {
-            const float2 one = state[n * W * 64 + lane];
-            by[n] = one.x == kNone ? 0.f : __builtin_amdgcn_exp2f((one.x - both) * a.scale);
-            total += one.y * by[n];
-        }
-        total += __shfl_xor(total, 32, 64);
-        if (row >= p.nq) return;
-        const float norm = total > 0.f ? 1.f / total : 0.f;
+            for (int n = 0; n < SETS; ++n) both = fmaxf(both, state[n * W * 64 + r].x);
 #pragma unroll
-        for (int n = 0; n < SETS; ++n) by[n] *= norm;
+            for (int n = 0; n < SETS; ++n) {
+                const float2 one = state[n * W * 64 + r];
+                const float by = one.x == kNone ? 0.f : __builtin_amdgcn_exp2f((one.x - both) * a.scale);
+                all += (one.y + state[n * W * 64 + r + 32].y) * by;
+                lo += area[(n * W * PARTS + c) * 64 + (r ^ c)] * by;
+                hi += area[(n * W * PARTS + c) * 64 + ((r + 32) ^ c)] * by;
+            }
+            const float norm = all > 0.f ? 1.f / all : 0.f;
+            f16x8 y;
 #pragma unroll
-        for (int j = 0; j < PARTS / SETS; ++j) {
-            const int i = set * (PARTS / SETS) + j;
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int n = 0; n < SETS; ++n) y += area[(n * W * PARTS + i) * 64 + lane] * by[n];
-            store(i, y);
+            for (int e = 0; e < 4; ++e) y[e] = (_Float16)(lo[e] * norm), y[4 + e] = (_Float16)(hi[e] * norm);
+            store(r, c, y);
         }
     }
 }
@@ -364,7 +391,8 @@ int64_t tiles_of(int64_t T_q, int64_t n_seqs, int64_t rows) { return T_q / rows 
 
 template <int D, int W, int SETS, int KEYS> hipError_t launch_dim(Prefill a, int64_t n_seqs, hipStream_t st)
 {
-    constexpr int tiles = SETS * 4 * KEYS * D * 2, join = SETS == 1 ? 0 : SETS * W * (D / 8 * 1024 + 512), bytes = tiles > join ? tiles : join;
+    constexpr int tiles = SETS * 4 * KEYS * D * 2, queries = 2 * KEYS * D * 2 + W * 32 * D * 2;
+    constexpr int join = SETS == 1 ? 0 : SETS * W * (D / 8 * 1024 + 512), most = tiles > join ? tiles : join, bytes = most > queries ? most : queries;
     if (hipError_t e = allow_dynamic_lds<attn_prefill_kernel<D, W, SETS, KEYS>>(bytes); e != hipSuccess) return e;
     a.tiles = (int)tiles_of(a.tokens_q, n_seqs, 32 * W);
     hipLaunchKernelGGL((attn_prefill_kernel<D, W, SETS, KEYS>), dim3((unsigned)((int64_t)a.tiles * a.heads)), dim3(64 * W * SETS), bytes, st, a);
