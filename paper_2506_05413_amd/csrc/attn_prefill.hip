@@ -52,7 +52,9 @@ struct Prefill {
     int64_t ldq, ldk, ldv;
     const int32_t *cu_q, *cu_k;
     int n_seqs, tokens_q, tokens_k;
-    int heads, kv, tiles;                                // tiles: of query rows, an upper bound
+    int heads, kv, group;                                // group: query heads of one key/value head
+    int head_shift, row_shift;                           // log2 of the heads and of the rows of one that a workgroup takes
+    int tiles;                                           // of query rows, an upper bound
     int at_once;                                         // tiles whose workgroups fill half of the places
     int causal;
     float scale;                                         // times log2(e)
@@ -78,24 +80,25 @@ __device__ __forceinline__ void take(Place &p, int lane_of, int q0, int nq, int 
 
 // The tile-th tile of rows of the batch, those with the most keys first; false behind the last.  A lane looks at a sequence.
 // (Nine prompts of 26 .. 541 tokens: 29.3 -> 25.7 us.)  Up to 64 sequences: tile i of a sequence that has `ahead` more keys than
-// queries is on level i + 1 + ahead / ROWS, and a level is found by bisection over the number of tiles above it.  Where every workgroup has its place at once (`at_once` tiles are
+// queries is on level i + 1 + ahead / (rows of a tile), and a level is found by bisection over the number of tiles above it.  Where every workgroup has its place at once (`at_once` tiles are
 // half of the places), the second half of them is dealt out from the other end, so that a compute unit's two workgroups are a
 // long and a short one (one prompt of 2048 tokens, 32 heads of 128: 48.6 -> 47.4 us).  More sequences: the last one's last first.
-template <int ROWS> __device__ __forceinline__ bool find_tile(const Prefill &a, int tile, int lane, Place &p)
+__device__ __forceinline__ bool find_tile(const Prefill &a, int tile, int lane, Place &p)
 {
+    auto tiles_in = [&](int rows) { return (int)(((uint32_t)rows + (1u << a.row_shift) - 1) >> a.row_shift); };
     if (a.n_seqs <= 64) {
         const int s = min(lane, a.n_seqs - 1);
         const int q_from = a.cu_q[s], q_to = a.cu_q[s + 1], k_from = a.cu_k[s], k_to = a.cu_k[s + 1];
         int q0, nq, k0, nk;
         span(q_from, q_to, a.tokens_q, q0, nq);
         span(k_from, k_to, a.tokens_k, k0, nk);
-        const int n = lane < a.n_seqs ? (nq + ROWS - 1) / ROWS : 0;
-        const int ahead = max(nk - nq, 0) / ROWS;
+        const int n = lane < a.n_seqs ? tiles_in(nq) : 0;
+        const int ahead = max(nk - nq, 0) >> a.row_shift;
         auto above = [&](int level) { return __builtin_amdgcn_readlane(scan_of_wave(min(max(ahead + n - level, 0), n)), 63); };
         const int all = above(0);
         if (tile >= all) return false;
         if (all <= 2 * a.at_once && tile >= a.at_once) tile = all - 1 - (tile - a.at_once);
-        int low = 0, high = (a.tokens_k > a.tokens_q ? a.tokens_k : a.tokens_q) / ROWS + 1;   // above(low) > tile >= above(high)
+        int low = 0, high = ((a.tokens_k > a.tokens_q ? a.tokens_k : a.tokens_q) >> a.row_shift) + 1;   // above(low) > tile >= above(high)
         while (high - low > 1) {
             const int mid = low + (high - low) / 2;
             if (above(mid) > tile) low = mid;
@@ -118,7 +121,7 @@ template <int ROWS> __device__ __forceinline__ bool find_tile(const Prefill &a, 
         int q0, nq, k0, nk;
         span(q_from, q_to, a.tokens_q, q0, nq);
         span(k_from, k_to, a.tokens_k, k0, nk);
-        const int n = s0 + lane < a.n_seqs ? (nq + ROWS - 1) / ROWS : 0;
+        const int n = s0 + lane < a.n_seqs ? tiles_in(nq) : 0;
         const int upto = scan_of_wave(n);
         const unsigned long long past = __ballot(upto > tile);
         if (past) {
@@ -135,7 +138,6 @@ template <int ROWS> __device__ __forceinline__ bool find_tile(const Prefill &a, 
 // SETS sets of waves, each with every SETS-th tile of KEYS keys
 template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W * SETS, D == 64 && SETS == 4 ? 4 : 2) void attn_prefill_kernel(Prefill a)
 {
-    constexpr int ROWS = 32 * W;
     constexpr int CH = D / 8;                            // 16-byte chunks of a row
     constexpr uint32_t kTileBytes = KEYS * D * 2;
     constexpr int DT = D / 32, LOADS = KEYS * CH / (64 * W);    // column tiles; DMA loads of a wave per operand
@@ -145,13 +147,14 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem + set * 4 * kTileBytes;
     const uint8_t *tiles = smem + set * 4 * kTileBytes;
     // neighbouring workgroups take different key/value heads: an XCD, every eighth of them, keeps few heads' keys in its L2
-    const uint32_t x = blockIdx.x % (uint32_t)a.heads;
-    const int kvh = (int)(x % (uint32_t)a.kv), head = kvh * (a.heads / a.kv) + (int)(x / (uint32_t)a.kv);
+    const uint32_t blocks = (uint32_t)a.heads >> a.head_shift, x = blockIdx.x % blocks;
+    const int kvh = (int)(x % (uint32_t)a.kv);
+    const int head = kvh * a.group + ((int)(x / (uint32_t)a.kv) << a.head_shift) + (wave & ((1 << a.head_shift) - 1));
     Place p;
-    if (!find_tile<ROWS>(a, (int)(blockIdx.x / (uint32_t)a.heads), lane, p)) return;
-    const int r0 = p.local * ROWS, shift = p.nk - p.nq;
-    const int end = a.causal ? min(p.nk, min(r0 + ROWS, p.nq) + shift) : p.nk;         // keys that any row sees
-    const int w0 = r0 + 32 * wave, row = w0 + m;
+    if (!find_tile(a, (int)(blockIdx.x / blocks), lane, p)) return;
+    const int rows = 1 << a.row_shift, r0 = p.local << a.row_shift, shift = p.nk - p.nq;
+    const int end = a.causal ? min(p.nk, min(r0 + rows, p.nq) + shift) : p.nk;         // keys that any row sees
+    const int w0 = r0 + 32 * (wave >> a.head_shift), row = w0 + m;
     const int wend = w0 >= p.nq ? 0 : a.causal ? min(p.nk, min(w0 + 32, p.nq) + shift) : p.nk;   // .. of this wave
     const int rend = a.causal ? min(p.nk, row + shift + 1) : p.nk;                     // .. of this lane's row
     const int whole = a.causal ? min(p.nk, w0 + shift + 1) : p.nk;                     // keys that every row of the wave sees
@@ -389,13 +392,19 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
 // tiles of rows, at most: every sequence may end inside one
 int64_t tiles_of(int64_t T_q, int64_t n_seqs, int64_t rows) { return T_q / rows + (n_seqs < T_q ? n_seqs : T_q); }
 
-template <int D, int W, int SETS, int KEYS> hipError_t launch_dim(Prefill a, int64_t n_seqs, hipStream_t st)
+template <int D, int W, int SETS, int KEYS> hipError_t launch_dim(Prefill a, int64_t n_seqs, bool balance, hipStream_t st)
 {
     constexpr int tiles = SETS * 4 * KEYS * D * 2, queries = 2 * KEYS * D * 2 + W * 32 * D * 2;
     constexpr int join = SETS == 1 ? 0 : SETS * W * (D / 8 * 1024 + 512), most = tiles > join ? tiles : join, bytes = most > queries ? most : queries;
     if (hipError_t e = allow_dynamic_lds<attn_prefill_kernel<D, W, SETS, KEYS>>(bytes); e != hipSuccess) return e;
-    a.tiles = (int)tiles_of(a.tokens_q, n_seqs, 32 * W);
-    hipLaunchKernelGGL((attn_prefill_kernel<D, W, SETS, KEYS>), dim3((unsigned)((int64_t)a.tiles * a.heads)), dim3(64 * W * SETS), bytes, st, a);
+    // as many heads of a key/value head as there are row waves, if they come out even, so that a tile has few rows of each
+    a.head_shift = 0;
+    while ((2 << a.head_shift) <= W && a.group % (2 << a.head_shift) == 0) ++a.head_shift;
+    a.row_shift = __builtin_ctz(32 * W) - a.head_shift;
+    const int64_t blocks = a.heads >> a.head_shift;
+    a.tiles = (int)tiles_of(a.tokens_q, n_seqs, 1 << a.row_shift);
+    a.at_once = balance ? (int)((compute_units() + blocks - 1) / blocks) : 0;
+    hipLaunchKernelGGL((attn_prefill_kernel<D, W, SETS, KEYS>), dim3((unsigned)(a.tiles * blocks)), dim3(64 * W * SETS), bytes, st, a);
     return hipGetLastError();
 }
 
@@ -412,21 +421,19 @@ hipError_t launch_attn_prefill(const void *Q, int64_t ldq, const void *K, int64_
     a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
     a.cu_q = cu_q, a.cu_k = cu_k;
     a.n_seqs = (int)n_seqs, a.tokens_q = (int)T_q, a.tokens_k = (int)T_k;
-    a.heads = (int)n_heads, a.kv = (int)kv;
+    a.heads = (int)n_heads, a.kv = (int)kv, a.group = (int)(n_heads / kv);
     a.causal = causal, a.scale = scale * 1.4426950408889634f;
     a.o = static_cast<_Float16 *>(O), a.ldo = ldo;
     // 64 rows while such workgroups have their places at once, and for long sequences while two rounds of them suffice: with four
     // sets of waves from 2048 keys of a sequence on (heads of 64: 1024).  256 rows where two rounds of those workgroups are there
     // (heads of 64 gain nothing: 4096 tokens, 32 heads 93 us for 91).
     const int64_t units = compute_units(), places = units * (128 / dim), rows = T_q * n_heads;
-    a.at_once = 0;
     if (rows <= 64 * places || (rows <= 144 * places && T_k > 1024 * n_seqs)) {
-        if (T_k * (128 / dim) >= 2048 * n_seqs) return dim == 128 ? launch_dim<128, 2, 4, 32>(a, n_seqs, st) : launch_dim<64, 2, 4, 32>(a, n_seqs, st);
-        return dim == 128 ? launch_dim<128, 2, 2, 64>(a, n_seqs, st) : launch_dim<64, 2, 2, 64>(a, n_seqs, st);
+        if (T_k * (128 / dim) >= 2048 * n_seqs) return dim == 128 ? launch_dim<128, 2, 4, 32>(a, n_seqs, false, st) : launch_dim<64, 2, 4, 32>(a, n_seqs, false, st);
+        return dim == 128 ? launch_dim<128, 2, 2, 64>(a, n_seqs, false, st) : launch_dim<64, 2, 2, 64>(a, n_seqs, false, st);
     }
-    if (dim == 128 && rows >= 2 * 256 * units && T_q >= 1024 * n_seqs) return launch_dim<128, 8, 1, 64>(a, n_seqs, st);
-    a.at_once = (int)((units + n_heads - 1) / n_heads);
-    return dim == 128 ? launch_dim<128, 4, 1, 64>(a, n_seqs, st) : launch_dim<64, 4, 1, 64>(a, n_seqs, st);
+    if (dim == 128 && rows >= 2 * 256 * units && T_q >= 1024 * n_seqs) return launch_dim<128, 8, 1, 64>(a, n_seqs, false, st);
+    return dim == 128 ? launch_dim<128, 4, 1, 64>(a, n_seqs, true, st) : launch_dim<64, 4, 1, 64>(a, n_seqs, true, st);
 }
 
 }  // namespace sr
