@@ -2,9 +2,9 @@
 //
 //   o_i = sum_j softmax(scale q_i . k_j) v_j      over the keys j of row i's own sequence, j <= i + (keys - queries) if causal
 //
-// A workgroup takes 32 query rows of one head per row wave and walks over their keys 64 at a time with running sums; keys and
-// values come into LDS by DMA, one tile ahead.  Both products run on 32 x 32 x 16 matrix instructions with the query row in the
-// columns:
+// A row wave takes 32 query rows of a head, a workgroup's row waves heads that share a key/value head or further rows, and walks
+// over their keys 64 (or 32) at a time with running sums; keys and values come into LDS by DMA, one tile ahead.  Both products run
+// on 32 x 32 x 16 matrix instructions with the query row in the columns:
 //
 //   S^T = K Q^T   lane (m, g) = (lane % 32, lane / 32) gets the scores of row m and of tokens 8 i + 4 g + (0 .. 3)
 //   O^T = V^T P^T its k-index is the token: the eight weights that a lane supplies per instruction are those of tokens
@@ -22,16 +22,18 @@
 // What bounds it: long prompts the power the chip may draw (8192 tokens, 32 heads of 128, causal: the clock is 1.83 GHz of 2.4 and
 // the matrix pipe busy for half of the cycles), the others the chain of a row's tiles.  Per 64 keys and SIMD, two waves there, the
 // products alone take 0.85 us, with the weights 1.05, with the reads from LDS 1.3; one wave takes 1.05.  Hence four shapes of
-// workgroup (us for one prompt of T tokens, 32 heads and 8 key/value heads of 128, causal; then 8 heads):
-//                                                            T = 512   1024   2048   4096   8192     2048   3000   4096
-//   8 row waves      a tile loaded once for 256 rows            19.2   31.1   56.9    141    518                     94
-//   4 row waves      128 rows, two workgroups on a unit         13.9   23.7   47.4    146    537              52     71
-//   2 x 2 sets       64 rows; the sets take every other         11.6   24.3   65.1    209    772     27.2     39     56
-//                    tile and meet in LDS at the end
-//   2 x 4 sets       tiles of 32 keys, two waves per SIMD       12.5   25.1                          25.5     34     53
+// workgroup (us; 32 and 8 heads of 128, causal, one prompt of T tokens; 8 and 8 heads; nine prompts of T tokens together):
+//                                               T = 512   1024   2048   4096   8192  |  3000   4096   6000  |   400   1000
+//   8 row waves  a tile loaded once for 256        17.2   29.5   57.5    138    515  |    69     93    134  |   7.3   14.7
+//   4 row waves  two workgroups on a unit          13.0   22.8   46.2    145         |    51     70    108  |   6.7   12.3
+//   2 x 2 sets   the sets take every other tile    10.7   22.1   60.9    200         |    37     55    114  |  10.7   18.2
+//                and meet in LDS at the end
+//   2 x 4 sets   tiles of 32 keys                  10.8   21.7   58.5    192         |    33     51    107  |  11.2   19.0
 // Products interleaved with the weights of the tile before (three tiles in flight) were 9 % slower at 8192 tokens and 15 % at
 // 1024, 64 rows per wave (one wave per SIMD) 30 % slower, and two halves of a workgroup that multiply and weigh in turn, by
 // barriers, 6 .. 30 % slower.
+#include <algorithm>
+
 #include "gemm_common.h"
 
 namespace sr {
@@ -392,14 +394,21 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
 // tiles of rows, at most: every sequence may end inside one
 int64_t tiles_of(int64_t T_q, int64_t n_seqs, int64_t rows) { return T_q / rows + (n_seqs < T_q ? n_seqs : T_q); }
 
+// Heads of a key/value head for the row waves of a workgroup: as many as come out even, so that a tile has few rows of each
+// (nine prompts of 2500 tokens, 32 and 8 heads 26.0 -> 22.5 us, sixty 27.5 -> 17.3; one prompt the same).
+int group_even(int group, int waves)
+{
+    int heads = 1;
+    while (2 * heads <= waves && group % (2 * heads) == 0) heads *= 2;
+    return heads;
+}
+
 template <int D, int W, int SETS, int KEYS> hipError_t launch_dim(Prefill a, int64_t n_seqs, bool balance, hipStream_t st)
 {
     constexpr int tiles = SETS * 4 * KEYS * D * 2, queries = 2 * KEYS * D * 2 + W * 32 * D * 2;
     constexpr int join = SETS == 1 ? 0 : SETS * W * (D / 8 * 1024 + 512), most = tiles > join ? tiles : join, bytes = most > queries ? most : queries;
     if (hipError_t e = allow_dynamic_lds<attn_prefill_kernel<D, W, SETS, KEYS>>(bytes); e != hipSuccess) return e;
-    // as many heads of a key/value head as there are row waves, if they come out even, so that a tile has few rows of each
-    a.head_shift = 0;
-    while ((2 << a.head_shift) <= W && a.group % (2 << a.head_shift) == 0) ++a.head_shift;
+    a.head_shift = __builtin_ctz(group_even(a.group, W));
     a.row_shift = __builtin_ctz(32 * W) - a.head_shift;
     const int64_t blocks = a.heads >> a.head_shift;
     a.tiles = (int)tiles_of(a.tokens_q, n_seqs, 1 << a.row_shift);
@@ -424,15 +433,18 @@ hipError_t launch_attn_prefill(const void *Q, int64_t ldq, const void *K, int64_
     a.heads = (int)n_heads, a.kv = (int)kv, a.group = (int)(n_heads / kv);
     a.causal = causal, a.scale = scale * 1.4426950408889634f;
     a.o = static_cast<_Float16 *>(O), a.ldo = ldo;
-    // 64 rows while such workgroups have their places at once, and for long sequences while two rounds of them suffice: with four
-    // sets of waves from 2048 keys of a sequence on (heads of 64: 1024).  256 rows where two rounds of those workgroups are there
-    // (heads of 64 gain nothing: 4096 tokens, 32 heads 93 us for 91).
-    const int64_t units = compute_units(), places = units * (128 / dim), rows = T_q * n_heads;
-    if (rows <= 64 * places || (rows <= 144 * places && T_k > 1024 * n_seqs)) {
-        if (T_k * (128 / dim) >= 2048 * n_seqs) return dim == 128 ? launch_dim<128, 2, 4, 32>(a, n_seqs, false, st) : launch_dim<64, 2, 4, 32>(a, n_seqs, false, st);
+    // Sets of waves over the keys while the workgroups of two row waves (load: how many there are for a place) are few for how
+    // long a row's keys are, four sets for long ones (heads of 64, which have two workgroups on a unit: where not even all
+    // places are taken).  Heads of 64 gain nothing from 256 rows a workgroup (4096 tokens, 32 heads 84 us for 85).
+    const int64_t units = compute_units();
+    const double rows = (double)T_q * n_heads, keys = (double)T_k / n_seqs;
+    const int share = group_even(a.group, 2);            // heads of such a workgroup
+    const double load = ((double)T_q + (n_seqs - 1.0) * (32 / share)) * n_heads / (64.0 * units * (128 / dim));
+    if (keys > 64 && load <= std::min(0.75 + keys / 700, 2.25)) {
+        if (keys >= 1024 && (dim == 128 || load <= 0.75)) return dim == 128 ? launch_dim<128, 2, 4, 32>(a, n_seqs, false, st) : launch_dim<64, 2, 4, 32>(a, n_seqs, false, st);
         return dim == 128 ? launch_dim<128, 2, 2, 64>(a, n_seqs, false, st) : launch_dim<64, 2, 2, 64>(a, n_seqs, false, st);
     }
-    if (dim == 128 && rows >= 2 * 256 * units && T_q >= 1024 * n_seqs) return launch_dim<128, 8, 1, 64>(a, n_seqs, false, st);
+    if (dim == 128 && rows >= 512.0 * units && T_q >= 2048 * n_seqs) return launch_dim<128, 8, 1, 64>(a, n_seqs, false, st);
     return dim == 128 ? launch_dim<128, 4, 1, 64>(a, n_seqs, true, st) : launch_dim<64, 4, 1, 64>(a, n_seqs, true, st);
 }
 

@@ -83,7 +83,9 @@ def test_one_prompt(gpu, T, H, KV, d):
 @pytest.mark.parametrize("nq,nk,H,KV,d", [([300], [300], 12, 3, 128), ([700, 650, 900, 80], [700, 1400, 900, 33], 24, 6, 128), ([2500], [2500], 56, 1, 128),
                                           ([1100, 1500], [1100, 1700], 60, 2, 128), ([700, 10, 650], [800, 10, 650], 40, 4, 64), ([140] * 70, [150] * 70, 8, 8, 128),
                                           ([1400], [1400], 18, 2, 128), ([5, 64, 1, 130, 0], [2050, 3000, 2200, 2500, 2300], 6, 2, 128), ([200, 77], [1200, 1111], 4, 2, 64),
-                                          ([10, 40, 3], [0, 6200, 5], 5, 5, 128), ([33, 300], [20, 2100], 3, 1, 64)])
+                                          ([10, 40, 3], [0, 6200, 5], 5, 5, 128), ([33, 300], [20, 2100], 3, 1, 64),
+                                          ([2200], [2200], 60, 4, 128), ([2200, 2300], [2200, 2300], 30, 5, 128), ([40] * 9, [45] * 9, 32, 8, 128),
+                                          ([300, 20, 150], [300, 20, 150], 24, 2, 64), ([7] * 100, [9] * 100, 16, 4, 64)])
 @pytest.mark.parametrize("causal", [True, False])
 def test_every_shape_of_workgroup(gpu, nq, nk, H, KV, d, causal):
     """Few rows (two or four sets of waves over the keys), more of them (128 rows a workgroup, with and without all of them at once, and
