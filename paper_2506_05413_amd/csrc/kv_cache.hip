@@ -7,8 +7,8 @@
 // Every product, sum and quotient comes out as rounded on its own: keys are rounded to fp16 and values next to a rounding
 // boundary take the code that the formula in fp32 gives, whoever evaluates it.
 //
-// Bound by its bytes where there are many tokens (16384 with 32 query heads and 8 key/value heads of 128, 4 bits: 363 MB in 80 us,
-// 4.5 TB/s; 2047 with the transform 14 us, 3.3 TB/s), else by the launch (one token 2.5 us).  Eight values (16 bytes) per lane,
+// Bound by its bytes where there are many tokens (16384 with 32 query heads and 8 key/value heads of 128, 4 bits: 387 MB in 75 us,
+// 5.1 TB/s; 2047 with the transform 13 us, 3.7 TB/s), else by the launch (one token 2.3 us).  Eight values (16 bytes) per lane,
 // D / 8 lanes per row, a row being one head of one token, query, key or value; the head's other half, the butterflies and the
 // range of a row are exchanged between those lanes with operand permutations, without LDS.
 #include "sr_common.h"
@@ -18,14 +18,18 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-union Eight { u32x4 v; uint32_t w[4]; __half h[8]; };
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+union Eight { u32x4 v; uint32_t w[4]; __half h[8]; f16x2 p[4]; };
 
-// lane ^ MASK inside a row of 16 lanes
+// Lane l of a row holds the eight values number l ^ 3 if bit 2 of l is set, else l: number ^ 4 then is in lane l ^ 7, which is one
+// exchange (l ^ 4 would be two).  Everything below goes by that number, called lane.
+__device__ __forceinline__ int number_of(int l) { return l ^ (l & 4 ? 3 : 0); }
+// number ^ MASK inside a row of 16 lanes
 template <int MASK, typename T> __device__ __forceinline__ T lane_xor(T v)
 {
     if constexpr (MASK == 1) return lane_perm<0xB1>(v);
     else if constexpr (MASK == 2) return lane_perm<0x4E>(v);
-    else if constexpr (MASK == 4) return lane_perm<0x1B>(lane_perm<0x141>(v));    // 7 - i, then 3 - i inside the quad
+    else if constexpr (MASK == 4) return lane_perm<0x141>(v);                     // lane 7 - l of eight
     else return lane_perm<0x128>(v);                                              // rotation by 8 of 16
 }
 
@@ -46,11 +50,8 @@ template <int MASK> __device__ __forceinline__ void butterfly(float (&v)[8], int
         : "v"(sign))
     if constexpr (MASK == 1) SR_STEP("quad_perm:[1,0,3,2]");
     else if constexpr (MASK == 2) SR_STEP("quad_perm:[2,3,0,1]");
-    else if constexpr (MASK == 8) SR_STEP("row_ror:8");
-    else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = fmaf(lane_xor<4>(v[e]), sign, v[e]);
-    }
+    else if constexpr (MASK == 4) SR_STEP("row_half_mirror");
+    else SR_STEP("row_ror:8");
 #undef SR_STEP
 }
 
@@ -149,8 +150,9 @@ template <int D> __device__ __forceinline__ uint32_t quantise_row(const Eight &x
 struct Append {
     const __half *q, *k, *v;
     int64_t ldq, ldk, ldv;
-    uint32_t rows;                       // tokens * (heads + 2 * kv)
+    uint32_t tokens;
     int heads, kv;
+    uint32_t q_waves, kv_waves;          // waves over the queries; over the keys, and over the values
     const int32_t *positions;
     const int64_t *slots;
     const float *table;
@@ -164,22 +166,41 @@ struct Append {
     int64_t ldqo, ldko;
 };
 
+// APART: a wave's rows are all queries, all keys or all values, so that what differs between those is scalar; else rows lie in the
+// order of the tokens.  Measured (us, apart / in order; 32 + 2 x 8 heads of 128): with the transform 1024 tokens 8.3 / 9.3, 2047
+// 13.0 / 13.8, 4096 23.5 / 24.9, 16384 95 / 95; without it 2047 10.6 / 11.2, 4096 19.6 / 20.4, 8192 41.4 / 41.4 (fp16 42.7 / 40.7),
+// 16384 79 / 75 (fp16 82 / 75).
 // (One row per group of lanes: two or four, on their way together, were 2 - 8 % slower up to 4096 tokens and 4 % faster at 16384.)
-template <int D, bool I4, bool PAIRS, bool HAD> __global__ __launch_bounds__(256) void rope_kv_append_kernel(Append a)
+template <int D, bool I4, bool PAIRS, bool HAD, bool APART> __global__ __launch_bounds__(256) void rope_kv_append_kernel(Append a)
 {
-    constexpr int LPR = D / 8, GROUPS = 256 / LPR;
-    const int lane = threadIdx.x & (LPR - 1);
-    const uint32_t per = a.heads + 2 * a.kv, first = blockIdx.x * (uint32_t)GROUPS, row = first + threadIdx.x / LPR;
-    if (row >= a.rows) return;
-    const uint32_t token0 = first / per, rest = row - token0 * per;
+    constexpr int LPR = D / 8, ROWS = 64 / LPR;          // rows of a wave
+    const int lane = number_of(threadIdx.x & (LPR - 1));
+    bool is_q, is_v;
+    uint32_t heads, first;                               // of the rows that this one is among: heads of a token, the wave's first row
+    if constexpr (APART) {
+        uint32_t wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        is_q = wave < a.q_waves, is_v = wave >= a.q_waves + a.kv_waves;
+        wave -= is_q ? 0 : is_v ? a.q_waves + a.kv_waves : a.q_waves;
+        if (wave >= a.kv_waves && is_v) return;
+        heads = is_q ? a.heads : a.kv, first = wave * ROWS;
+    } else {
+        heads = a.heads + 2 * a.kv, first = blockIdx.x * (4 * ROWS);
+    }
+    const uint32_t token0 = first / heads, rest = first - token0 * heads + (APART ? threadIdx.x & 63 : threadIdx.x) / LPR;
     // (the quotient, 32 at most, is half a row away from the next whole number)
-    const uint32_t on = (uint32_t)(((float)rest + 0.5f) * __builtin_amdgcn_rcpf((float)per)), token = token0 + on;
-    const int head = (int)(rest - on * per);
-    const bool is_q = head < a.heads, is_v = head >= a.heads + a.kv;
-    const int h = is_q ? head : is_v ? head - a.heads - a.kv : head - a.heads;
-    const __half *src = is_q ? a.q + token * a.ldq : is_v ? a.v + token * a.ldv : a.k + token * a.ldk;
+    const uint32_t on = (uint32_t)(((float)rest + 0.5f) * __builtin_amdgcn_rcpf((float)heads)), token = token0 + on;
+    if (token >= a.tokens) return;
+    int h = (int)(rest - on * heads);
+    if constexpr (!APART) {
+        is_q = h < a.heads, is_v = h >= a.heads + a.kv;
+        h -= is_q ? 0 : is_v ? a.heads + a.kv : a.heads;
+    }
+    // (in order, the rows' addresses from the start)
+    const uint32_t base = APART ? token0 : token, off = APART ? on : 0, column = h * D + 8 * lane;
+    const __half *src = is_q ? a.q + base * a.ldq : is_v ? a.v + base * a.ldv : a.k + base * a.ldk;
+    const int64_t ld = is_q ? a.ldq : is_v ? a.ldv : a.ldk;
     Eight x;
-    x.v = *reinterpret_cast<const u32x4 *>(src + (int64_t)h * D + 8 * lane);
+    x.v = *reinterpret_cast<const u32x4 *>(src + (off * ld + column));
     const int64_t slot = is_q ? 0 : a.slots[token];
     if (!is_v && (a.table || HAD)) {
         float v[8];
@@ -191,16 +212,16 @@ template <int D, bool I4, bool PAIRS, bool HAD> __global__ __launch_bounds__(256
         }
         if constexpr (HAD) hadamard_row<D>(v, lane);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            asm("" : "+v"(v[e]));                        // a number of fp32: the last product is not to be rounded to fp16 at once
-            x.h[e] = __float2half_rn(v[e]);
+        for (int e = 0; e < 8; e += 2) {
+            asm("" : "+v"(v[e]), "+v"(v[e + 1]));        // numbers of fp32: the last product is not to be rounded to fp16 at once
+            x.p[e / 2] = f16x2{(_Float16)v[e], (_Float16)v[e + 1]};
         }
     }
     if (is_q) {
-        *reinterpret_cast<u32x4 *>(a.qo + token * a.ldqo + (int64_t)h * D + 8 * lane) = x.v;
+        *reinterpret_cast<u32x4 *>(a.qo + base * a.ldqo + (off * a.ldqo + column)) = x.v;
         return;
     }
-    if (!is_v && a.ko) *reinterpret_cast<u32x4 *>(a.ko + token * a.ldko + (int64_t)h * D + 8 * lane) = x.v;
+    if (!is_v && a.ko) *reinterpret_cast<u32x4 *>(a.ko + base * a.ldko + (off * a.ldko + column)) = x.v;
     if (slot < 0 || slot >= a.n_slots) return;
     // page-major, then head, then token of the page
     const int64_t at = (((slot >> a.page_shift) * a.kv + h) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
@@ -289,15 +310,26 @@ template <int D, bool I4> hipError_t gather_dim(const Gather &a, hipStream_t st)
 
 inline int shift_of(int64_t page) { return __builtin_ctzll((unsigned long long)page); }
 
+template <int D, bool I4, bool APART> hipError_t append_rows(Append a, bool pairs, bool had, hipStream_t st)
+{
+    constexpr unsigned rows = 64 / (D / 8);              // of a wave
+    a.q_waves = (a.tokens * (unsigned)a.heads + rows - 1) / rows;
+    a.kv_waves = (a.tokens * (unsigned)a.kv + rows - 1) / rows;
+    const unsigned waves = APART ? a.q_waves + 2 * a.kv_waves : (a.tokens * (unsigned)(a.heads + 2 * a.kv) + rows - 1) / rows;
+    const dim3 grid((waves + 3) / 4), block(256);
+    if constexpr (!APART) {
+        if (pairs) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, true, false, APART>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, false, false, APART>), grid, block, 0, st, a);
+    } else if (pairs && had) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, true, true, APART>), grid, block, 0, st, a);
+    else if (pairs) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, true, false, APART>), grid, block, 0, st, a);
+    else if (had) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, false, true, APART>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, false, false, APART>), grid, block, 0, st, a);
+    return hipGetLastError();
+}
 template <int D, bool I4> hipError_t append_dim(const Append &a, bool pairs, bool had, hipStream_t st)
 {
-    constexpr unsigned rows = 256 / (D / 8);
-    const dim3 grid((a.rows + rows - 1) / rows), block(256);
-    if (pairs && had) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, true, true>), grid, block, 0, st, a);
-    else if (pairs) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, true, false>), grid, block, 0, st, a);
-    else if (had) hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, false, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((rope_kv_append_kernel<D, I4, false, false>), grid, block, 0, st, a);
-    return hipGetLastError();
+    const bool apart = had || (int64_t)a.tokens * (a.heads + 2 * a.kv) <= 1024 * (int64_t)compute_units();
+    return apart ? append_rows<D, I4, true>(a, pairs, had, st) : append_rows<D, I4, false>(a, pairs, had, st);
 }
 
 }  // namespace
@@ -310,7 +342,7 @@ hipError_t launch_rope_kv_append(const void *Q, int64_t ldq, const void *K, int6
     Append a;
     a.q = static_cast<const __half *>(Q), a.k = static_cast<const __half *>(K), a.v = static_cast<const __half *>(V);
     a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
-    a.rows = (uint32_t)(T * (n_heads + 2 * c.heads));
+    a.tokens = (uint32_t)T;
     a.heads = (int)n_heads, a.kv = (int)c.heads;
     a.positions = positions, a.slots = slots, a.table = cos_sin;
     a.max_pos = (int)max_pos, a.clip = clip;
