@@ -8,7 +8,7 @@
  *
  * The conventions of smoothrot.h hold (device pointers, stream, statuses, no allocation, 16-byte aligned bases, row strides
  * multiples of 8 where the elements are fp16), but for shapes: head_dim is 64 or 128 (SR_ERR_ARG otherwise), any number of
- * tokens, sequences and heads, n_heads a multiple of n_kv_heads (query head h reads key/value head
+ * tokens, sequences and heads (heads below 65536), n_heads a multiple of n_kv_heads (query head h reads key/value head
  * h / (n_heads / n_kv_heads)).  Rows of several heads lie one head after the other, [tokens, heads * head_dim].
  */
 #ifndef SMOOTHROT_ATTENTION_H

@@ -317,6 +317,7 @@ int sr_kv_quant_asym(const void *X_f16, int64_t rows, int64_t D, int64_t ldx, in
 // ---- paged cache and attention ----------------------------------------------------------------------------------------
 static bool head_dim_ok(int64_t d) { return d == 64 || d == 128; }
 
+static constexpr int64_t kMostHeads = 1 << 16;             // kernels divide rows by heads in fp32
 static int check_cache(const sr_kv_cache *cache, sr::KvCache &c)
 {
     if (!cache) return SR_ERR_NULL;
@@ -324,7 +325,7 @@ static int check_cache(const sr_kv_cache *cache, sr::KvCache &c)
     if (!head_dim_ok(cache->head_dim)) return SR_ERR_ARG;
     if (!sr::is_pow2(cache->page_size) || cache->page_size < 16 || cache->page_size > (1 << 20)) return SR_ERR_ARG;
     if (cache->n_pages < 1 || cache->n_pages >= ((int64_t)1 << 31) || cache->n_pages >= ((int64_t)1 << 40) / cache->page_size ||
-        cache->n_kv_heads < 1 || cache->n_kv_heads >= (1 << 20))
+        cache->n_kv_heads < 1 || cache->n_kv_heads >= kMostHeads)
         return SR_ERR_SHAPE;
     c.i4 = cache->type == SR_KV_I4;
     if (!cache->K || !cache->V || (c.i4 && (!cache->K_params || !cache->V_params))) return SR_ERR_NULL;
@@ -336,7 +337,7 @@ static int check_cache(const sr_kv_cache *cache, sr::KvCache &c)
 }
 static bool heads_fit(int64_t n_heads, int64_t n_kv_heads)
 {
-    return n_kv_heads >= 1 && n_heads >= n_kv_heads && n_heads < (1 << 20) && n_heads % n_kv_heads == 0;
+    return n_kv_heads >= 1 && n_heads >= n_kv_heads && n_heads < kMostHeads && n_heads % n_kv_heads == 0;
 }
 static bool scale_ok(float scale) { return scale > 0.f && scale <= 0x1p64f; }            // scores stay finite
 
@@ -348,7 +349,7 @@ int sr_rope_kv_append(const void *Q_f16, int64_t ldq, const void *K_f16, int64_t
     sr::KvCache c;
     if (const int e = check_cache(cache, c)) return e;
     const int64_t dq = n_heads * c.dim, dk = c.heads * c.dim;
-    if (T < 0 || n_heads < 0 || n_heads >= (1 << 20) || ldk < dk || ldv < dk || (n_heads && (ldq < dq || ldqo < dq)) || (K_out && ldko < dk))
+    if (T < 0 || n_heads < 0 || n_heads >= kMostHeads || ldk < dk || ldv < dk || (n_heads && (ldq < dq || ldqo < dq)) || (K_out && ldko < dk))
         return SR_ERR_SHAPE;
     if (T >= (1 << 27) || T * (n_heads + 2 * c.heads) >= (1 << 27)) return SR_ERR_SHAPE;
     if (flags & ~(SR_ROPE_PAIRS | SR_ROPE_HADAMARD) || (c.i4 && !(clip > 0.f && clip <= 1.f))) return SR_ERR_ARG;

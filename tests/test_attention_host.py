@@ -33,7 +33,7 @@ def cache(**changed):
 BAD_CACHES = [(dict(type=2), sr.SR_ERR_ARG), (dict(type=-1), sr.SR_ERR_ARG), (dict(head_dim=96), sr.SR_ERR_ARG), (dict(head_dim=0), sr.SR_ERR_ARG),
               (dict(page_size=8), sr.SR_ERR_ARG), (dict(page_size=24), sr.SR_ERR_ARG), (dict(page_size=0), sr.SR_ERR_ARG), (dict(page_size=-16), sr.SR_ERR_ARG),
               (dict(page_size=1 << 21), sr.SR_ERR_ARG), (dict(n_pages=0), sr.SR_ERR_SHAPE), (dict(n_pages=1 << 31), sr.SR_ERR_SHAPE),
-              (dict(n_pages=1 << 30, page_size=1 << 20), sr.SR_ERR_SHAPE), (dict(n_kv_heads=0), sr.SR_ERR_SHAPE), (dict(n_kv_heads=-2), sr.SR_ERR_SHAPE),
+              (dict(n_pages=1 << 30, page_size=1 << 20), sr.SR_ERR_SHAPE), (dict(n_kv_heads=0), sr.SR_ERR_SHAPE), (dict(n_kv_heads=-2), sr.SR_ERR_SHAPE), (dict(n_kv_heads=1 << 16), sr.SR_ERR_SHAPE),
               (dict(K=None), sr.SR_ERR_NULL), (dict(V=None), sr.SR_ERR_NULL), (dict(K_params=None), sr.SR_ERR_NULL), (dict(V_params=None), sr.SR_ERR_NULL),
               (dict(K=A + 8), sr.SR_ERR_ALIGN), (dict(V=A + 4), sr.SR_ERR_ALIGN), (dict(K_params=A + 8), sr.SR_ERR_ALIGN), (dict(V_params=A + 4), sr.SR_ERR_ALIGN)]
 
@@ -81,7 +81,7 @@ NAN, INF = float("nan"), float("inf")
 
 
 @pytest.mark.parametrize("changed,status", [
-    (dict(T=-1), sr.SR_ERR_SHAPE), (dict(H=-1), sr.SR_ERR_SHAPE), (dict(ldq=1016), sr.SR_ERR_SHAPE), (dict(ldqo=1016), sr.SR_ERR_SHAPE),
+    (dict(T=-1), sr.SR_ERR_SHAPE), (dict(H=-1), sr.SR_ERR_SHAPE), (dict(H=1 << 16, ldq=1 << 24, ldqo=1 << 24), sr.SR_ERR_SHAPE), (dict(ldq=1016), sr.SR_ERR_SHAPE), (dict(ldqo=1016), sr.SR_ERR_SHAPE),
     (dict(ldk=248), sr.SR_ERR_SHAPE), (dict(ldv=248), sr.SR_ERR_SHAPE), (dict(Ko=A, ldko=248), sr.SR_ERR_SHAPE), (dict(T=1 << 27), sr.SR_ERR_SHAPE),
     (dict(T=1 << 24), sr.SR_ERR_SHAPE), (dict(flags=4), sr.SR_ERR_ARG), (dict(clip=0.0), sr.SR_ERR_ARG), (dict(clip=1.01), sr.SR_ERR_ARG), (dict(clip=NAN), sr.SR_ERR_ARG),
     (dict(max_pos=0), sr.SR_ERR_SHAPE), (dict(max_pos=1 << 31), sr.SR_ERR_SHAPE), (dict(K=None), sr.SR_ERR_NULL), (dict(V=None), sr.SR_ERR_NULL),
@@ -128,7 +128,7 @@ def test_decode_workspace():
 @pytest.mark.parametrize("changed,status", [
     (dict(d=96), sr.SR_ERR_ARG), (dict(d=0), sr.SR_ERR_ARG), (dict(scale=0.0), sr.SR_ERR_ARG), (dict(scale=-0.5), sr.SR_ERR_ARG), (dict(scale=NAN), sr.SR_ERR_ARG), (dict(scale=INF), sr.SR_ERR_ARG), (dict(scale=2e19), sr.SR_ERR_ARG),
     (dict(n=-1), sr.SR_ERR_SHAPE), (dict(Tq=-1), sr.SR_ERR_SHAPE), (dict(Tk=-1), sr.SR_ERR_SHAPE), (dict(Tq=1 << 31), sr.SR_ERR_SHAPE), (dict(Tk=1 << 31), sr.SR_ERR_SHAPE),
-    (dict(H=0), sr.SR_ERR_SHAPE), (dict(H=7), sr.SR_ERR_SHAPE), (dict(KV=0), sr.SR_ERR_SHAPE), (dict(KV=16), sr.SR_ERR_SHAPE),
+    (dict(H=1 << 16, ldq=1 << 22, ldo=1 << 22), sr.SR_ERR_SHAPE), (dict(H=0), sr.SR_ERR_SHAPE), (dict(H=7), sr.SR_ERR_SHAPE), (dict(KV=0), sr.SR_ERR_SHAPE), (dict(KV=16), sr.SR_ERR_SHAPE),
     (dict(ldq=1016), sr.SR_ERR_SHAPE), (dict(ldo=1016), sr.SR_ERR_SHAPE), (dict(ldk=248), sr.SR_ERR_SHAPE), (dict(ldv=248), sr.SR_ERR_SHAPE),
     (dict(ldq=1 << 23), sr.SR_ERR_SHAPE), (dict(ldk=1 << 23), sr.SR_ERR_SHAPE), (dict(ldv=1 << 23), sr.SR_ERR_SHAPE), (dict(ldo=1 << 23), sr.SR_ERR_SHAPE),
     (dict(n=1 << 30, Tq=(1 << 31) - 1), sr.SR_ERR_SHAPE), (dict(Q=None), sr.SR_ERR_NULL), (dict(K=None), sr.SR_ERR_NULL), (dict(V=None), sr.SR_ERR_NULL), (dict(O=None), sr.SR_ERR_NULL),
