@@ -104,6 +104,13 @@ def test_append_shapes(gpu, T, H, KV, d, page, i4):
     check_append(gpu, T, H, KV, d, page, i4, False, T % 2 == 0, clip=1.0 if T == 5 else 0.95, seed=9)
 
 
+@pytest.mark.parametrize("T,H,KV,d,i4,pairs,hadamard", [(5501, 40, 4, 128, True, False, False), (6001, 36, 4, 64, False, False, False), (5801, 31, 7, 64, True, True, False),
+                                                        (5601, 41, 3, 128, False, True, False), (5503, 40, 4, 128, True, False, True)])
+def test_append_of_many_rows(gpu, T, H, KV, d, i4, pairs, hadamard):
+    """From 262144 rows on they are dealt out in the order of the tokens, unless the transform is asked for."""
+    check_append(gpu, T, H, KV, d, 64, i4, pairs, hadamard, seed=3)
+
+
 def test_append_without_rotation(gpu):
     check_append(gpu, 19, 4, 2, 128, 16, True, False, False, with_table=False, with_k_out=False)
     check_append(gpu, 19, 4, 2, 64, 16, False, False, True, with_table=False)
