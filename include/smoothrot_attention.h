@@ -111,7 +111,7 @@ SR_API int sr_attn_decode(const void *Q_f16, int64_t ldq, int64_t n_seqs, int64_
  *   cu_q, cu_k     int32 [n_seqs + 1]: sequence s holds rows cu_q[s] .. cu_q[s + 1] - 1 of Q and cu_k[s] .. of K and V (ascending;
  *                  cut to [0, T_q] and [0, T_k]).  Rows of no sequence are left as they were.
  *   scale          0 < scale <= 2^64
- *   O_f16          out, fp16 [T_q, n_heads * head_dim], row stride ldo
+ *   O_f16          out, fp16 [T_q, n_heads * head_dim], row stride ldo.  May be Q_f16 (same stride).
  * T_q, T_k < 2^31, row strides < 2^23, (T_q / 64 + n_seqs) * n_heads < 2^31.  A non-finite key or value reaches rows of its own
  * sequence only.
  */

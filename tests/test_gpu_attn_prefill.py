@@ -74,6 +74,16 @@ def test_other_numbers_of_keys(gpu, d, causal):
         assert (got[at[5]:at[5] + 130] == 0).all()
 
 
+def test_no_keys_at_all_and_output_over_the_queries(gpu):
+    q, k, v = make([5, 40], [5, 40], 4, 2, 128)
+    assert (run(gpu, q, k[:0], v[:0], [5, 40], [0, 0]) == 0).all() and (run(gpu, q, k[:0], v[:0], [5, 40], [0, 0], False) == 0).all()
+    Q, cu = dev(q.reshape(45, -1)), dev(ends([5, 40]))
+    want = run(gpu, q, k, v, [5, 40], [5, 40])
+    assert gpu.sr_attn_prefill(Q, dev(k.reshape(45, -1)), dev(v.reshape(45, -1)), cu, cu, 128, O=Q).data_ptr() == Q.data_ptr()
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(Q.cpu().numpy().reshape(45, 4, 128), want)
+
+
 @pytest.mark.parametrize("T,H,KV,d", [(1, 32, 8, 128), (1000, 4, 1, 128), (777, 2, 2, 64)])
 def test_one_prompt(gpu, T, H, KV, d):
     q, k, v = make([T], [T], H, KV, d, seed=T)
