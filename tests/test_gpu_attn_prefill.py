@@ -42,7 +42,7 @@ def check(got, q, k, v, nq, nk, causal, scale, what=""):
 
 def run(sr, q, k, v, nq, nk, causal=True, scale=None, **more):
     T, H, d = q.shape
-    got = sr.sr_attn_prefill(dev(q.reshape(T, -1)), dev(k.reshape(len(k), -1)), dev(v.reshape(len(v), -1)), dev(ends(nq)), dev(ends(nk)), d, causal, scale, **more)
+    got = sr.sr_attn_prefill(dev(q.reshape(T, -1)), dev(k.reshape(len(k), k.shape[1] * d)), dev(v.reshape(len(v), v.shape[1] * d)), dev(ends(nq)), dev(ends(nk)), d, causal, scale, **more)
     torch.cuda.synchronize()
     return got.cpu().numpy().reshape(T, H, d)
 
