@@ -4,9 +4,10 @@
 //
 // Bound by the bytes of the cache where it is long (4 bits, 8 key/value heads of 128: 64 sequences of 0 .. 8192 tokens, 294 MB, in
 // 55 us = 5.3 TB/s; fp16, 32 heads of 64: 24 sequences of 2000 tokens, 241 MB, in 45 us), else by the launch and the chain of
-// loads of one sequence (130 tokens 5 us, 65000 tokens, 75 MB, 20 us with the join).  A workgroup takes one key/value head (up to 16 of the query heads that share it) and runs of
-// tokens; its four waves walk over tiles of 32 tokens with a running maximum and sum, and meet in LDS.  Both products run on
-// 16 x 16 x 32 matrix instructions with the query head in the columns:
+// loads and tiles of one sequence (130 tokens 5.6 us, 0.8 us for a wave's tile; 65000 tokens, 75 MB, 21 us with the join).  A workgroup
+// takes one key/value head (up to 16 of the query heads that share it) and runs of tokens; its waves walk over tiles of 32 tokens
+// with a running maximum and sum, and meet in LDS.  Both products run on 16 x 16 x 32 matrix instructions with the query head in
+// the columns:
 //
 //   S^T = K Q^T   rows = tokens: lane (n, g) = (lane % 16, lane / 16) holds token n of the operand and gets tokens 4 g + r
 //   O^T = V^T P^T its k-index is the token: lane (n, g) supplies the eight tokens 4 g + r of two halves of the tile, which are
@@ -298,10 +299,11 @@ template <int D, bool I4> struct Rows {
 };
 
 // Tokens [first, last) of sequence b over a wave's tiles, `smem` the wave's own stages (4 bits).
-template <int D, bool I4>
+template <int D, bool I4, int WAVES>
 __device__ __forceinline__ void walk(const Decode &a, Rows<D, I4> &rows, int b, int h, int first, int last, uint8_t *smem, int wave, int lane)
 {
     using T = Tile<D, I4>;
+    constexpr int ROUND = WAVES * kTile;
     const int n = lane & 15, g = lane >> 4;
     // (constant while the kernel runs: scalar loads, which the vector counter does not see)
     const auto *table = (const __attribute__((address_space(4))) int32_t *)(uintptr_t)(a.table + (int64_t)b * a.ld_table);
@@ -386,30 +388,30 @@ __device__ __forceinline__ void walk(const Decode &a, Rows<D, I4> &rows, int b, 
         Where w = where(t0, pages_of(t0));
         uint32_t there = w.there, there_next = 0;
         load(0, w);
-        if (t0 + kRound < last) {
-            w = where(t0 + kRound, pages_of(t0 + kRound));
+        if (t0 + ROUND < last) {
+            w = where(t0 + ROUND, pages_of(t0 + ROUND));
             there_next = w.there;
             load(1, w);
         }
-        Pages next = pages_of(t0 + 2 * kRound);
-        for (int slot = 0; t0 < last; t0 += kRound, slot ^= 1) {
+        Pages next = pages_of(t0 + 2 * ROUND);
+        for (int slot = 0; t0 < last; t0 += ROUND, slot ^= 1) {
             T t;
-            if (t0 + kRound < last) wait_vmcnt<LOADS>();
+            if (t0 + ROUND < last) wait_vmcnt<LOADS>();
             else wait_vmcnt<0>();
             fetch(t, slot);
             const uint32_t here = there;
             there = there_next;
-            if (t0 + 2 * kRound < last) {
+            if (t0 + 2 * ROUND < last) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                w = where(t0 + 2 * kRound, next);
+                w = where(t0 + 2 * ROUND, next);
                 there_next = w.there;
                 load(slot, w);
-                next = pages_of(t0 + 3 * kRound);
+                next = pages_of(t0 + 3 * ROUND);
             }
             rows.use(t, t0, last, here, n, g);
         }
     } else {
-        for (; t0 < last; t0 += kRound) {
+        for (; t0 < last; t0 += ROUND) {
             T t;
             const Where w = where(t0, pages_of(t0));
 #pragma unroll
@@ -448,9 +450,9 @@ template <int D> __device__ __forceinline__ void store_row(_Float16 *dst, f32x4 
     *reinterpret_cast<u32x2 *>(dst) = y.v;
 }
 
-template <int D, bool I4> __global__ __launch_bounds__(kWaves * 64, 2) void attn_decode_kernel(Decode a)
+template <int D, bool I4, int WAVES> __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void attn_decode_kernel(Decode a)
 {
-    constexpr int C = D / 16;
+    constexpr int C = D / 16, ROUND = WAVES * kTile;     // (kRound where there are shares)
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -466,17 +468,17 @@ template <int D, bool I4> __global__ __launch_bounds__(kWaves * 64, 2) void attn
         if (b == a.n_seqs) return;
     }
     for (;;) {
-        const int len = length_of(a, b), rounds = (len + kRound - 1) / kRound;
+        const int len = length_of(a, b), rounds = (len + ROUND - 1) / ROUND;
         const int r0 = max(from - before, 0), r1 = a.shares ? min(to - before, rounds) : rounds;
         const bool whole = r0 == 0 && r1 == rounds;
         Rows<D, I4> rows;
         rows.begin(a.q + (int64_t)b * a.ldq + (int64_t)(head0 + n) * D, n < n_rows, g, a.scale);
-        walk<D, I4>(a, rows, b, h, r0 * kRound, min(r1 * kRound, len), smem + wave * (2 * Stage<D>::BYTES), wave, lane);
+        walk<D, I4, WAVES>(a, rows, b, h, r0 * ROUND, min(r1 * ROUND, len), smem + wave * (2 * Stage<D>::BYTES), wave, lane);
         __syncthreads();                                 // the stages' area is used again
 
-        // the four waves meet: acc[j][r] of lane (n, g) is column d = C (4 g + r) + j of query row n
-        float(*s_top)[16] = reinterpret_cast<float(*)[16]>(smem), (*s_total)[16] = s_top + kWaves;
-        float(*s_acc)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(s_total + kWaves);
+        // the waves meet: acc[j][r] of lane (n, g) is column d = C (4 g + r) + j of query row n
+        float(*s_top)[16] = reinterpret_cast<float(*)[16]>(smem), (*s_total)[16] = s_top + WAVES;
+        float(*s_acc)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(s_total + WAVES);
         const float back = I4 ? __builtin_amdgcn_exp2f(rows.lift) : 1.f, total = sum_of_groups(rows.total) * back, zsum = sum_of_groups(rows.zsum);
         if (g == 0) s_top[wave][n] = rows.top, s_total[wave][n] = total;
         if (n < n_rows) {
@@ -491,16 +493,16 @@ template <int D, bool I4> __global__ __launch_bounds__(kWaves * 64, 2) void attn
                 }
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < n_rows * (D / 4); i += kWaves * 64) {
+        for (int i = threadIdx.x; i < n_rows * (D / 4); i += WAVES * 64) {
             const int m = i / (D / 4), d = 4 * (i % (D / 4));
             float most = s_top[0][m];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) most = fmaxf(most, s_top[w][m]);
+            for (int w = 1; w < WAVES; ++w) most = fmaxf(most, s_top[w][m]);
             const float base = most == kNone ? 0.f : most;
             f32x4 sum = 0.f;
             float all = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float e = __builtin_amdgcn_exp2f(s_top[w][m] - base);
                 sum += e * *reinterpret_cast<const f32x4 *>(&s_acc[w][m][d]);
                 all += e * s_total[w][m];
@@ -599,14 +601,26 @@ template <int D, int PARTS> __global__ __launch_bounds__(256) void attn_join_ker
     store_row<D>(a.o + (int64_t)b * a.ldo + (int64_t)head * D + d, sum, all);
 }
 
+template <int D, bool I4, int WAVES> hipError_t launch_waves(const Decode &a, hipStream_t st)
+{
+    constexpr int meet = WAVES * 16 * (D + 4 + 2) * 4, stages = I4 ? WAVES * 2 * Stage<D>::BYTES : 0;
+    constexpr int lds = meet > stages ? meet : stages;
+    static_assert(lds <= 160 * 1024, "within what a workgroup may have");
+    if constexpr (lds > 65536)
+        if (hipError_t e = allow_dynamic_lds<attn_decode_kernel<D, I4, WAVES>>(lds); e != hipSuccess) return e;
+    const dim3 grid((unsigned)(a.shares ? a.shares : a.n_seqs) * (unsigned)a.per_seq);
+    hipLaunchKernelGGL((attn_decode_kernel<D, I4, WAVES>), grid, dim3(WAVES * 64), lds, st, a);
+    return hipGetLastError();
+}
+
+// Eight waves where a workgroup has a unit to itself and a whole sequence to do (4 bits; us, 4 waves / 8: one sequence of 500 tokens 7.6
+// / 7.1, 16 of 2000 17.5 / 14.3, 32 of up to 2000 17.8 / 14.8; 64 of 500 10.2 / 13.0.  Sixteen 9.4, 17.7, 20.2 and 21.  fp16 gains nothing:
+// 32 of 1000 19.6 / 19.4).
 template <int D, bool I4> hipError_t launch_shares(const Decode &a, hipStream_t st)
 {
-    constexpr int meet = kWaves * 16 * (D + 4 + 2) * 4, stages = I4 ? kWaves * 2 * Stage<D>::BYTES : 0;
-    constexpr int lds = meet > stages ? meet : stages;
-    static_assert(lds <= 65536, "within the default limit of dynamic LDS");
-    const dim3 grid((unsigned)(a.shares ? a.shares : a.n_seqs) * (unsigned)a.per_seq);
-    hipLaunchKernelGGL((attn_decode_kernel<D, I4>), grid, dim3(kWaves * 64), lds, st, a);
-    return hipGetLastError();
+    if constexpr (I4)
+        if (!a.shares && (int64_t)a.n_seqs * a.per_seq <= compute_units() && a.max_len > 2 * kRound) return launch_waves<D, I4, 8>(a, st);
+    return launch_waves<D, I4, 4>(a, st);
 }
 
 template <int D> hipError_t launch_join(const Decode &a, hipStream_t st)
@@ -619,19 +633,19 @@ template <int D> hipError_t launch_join(const Decode &a, hipStream_t st)
 }
 
 // Shares of the sequences of one key/value head and row tile; 0: a workgroup per sequence does it all, which needs no second
-// kernel (4 us) and no change from one sequence to the next, but takes as long as the longest sequence: 0.8 us a round (4 bits;
-// fp16, which keeps one tile of a wave on its way, 1.6), or what the bytes take.  Measured (us, shares / a workgroup each):
-//   4 bits, 8 key/value heads of 128:  1 sequence of 500 tokens 8.7 / 7.2, 768 8.7 / 8.6, 1000 8.7 / 10.2;  8 of 500 9.3 / 7.5, 1000
-//     10.4 / 10.7;  16 of up to 1000 13.8 / 10.7, 2000 16.7 / 17.0;  32 of up to 2000 21.5 / 17.6, 3000 22.5 / 23.4;  64 of up to 2000
-//     26.6 / 23.0, 8192 56 / 95;  128 of up to 2000 45 / 37, 4096 60 / 67
+// kernel (4 us) and no change from one sequence to the next, but takes as long as the longest sequence: 0.8 us a round (4 bits; with
+// eight waves 0.75; fp16, which keeps one tile of a wave on its way, 1.6), or what the bytes take.  Measured (us, shares / a workgroup each):
+//   4 bits, 8 key/value heads of 128:  1 sequence of 500 tokens 8.7 / 7.1, 896 8.8 / 8.5, 1000 9.2 / 9.4;  8 of 1000 10.6 / 9.7, 1300
+//     14.0 / 11.1, up to 2000 12.9 / 14.0;  16 of 2000 17.8 / 14.7, up to 3000 19.7 / 18.7, 4000 21.1 / 22.9;  32 of up to 3000 22.1 / 19.6,
+//     4000 24.1 / 24.0;  64 of up to 2000 26.6 / 23.0, 8192 56 / 95;  128 of up to 2000 45 / 37, 4096 60 / 67
 //   fp16:  1 of 384 8.7 / 7.2;  8 of 500 10.2 / 11.2;  32 of 500 17.4 / 13.5;  64 of up to 1000 30.5 / 33.5
 int shares_of(int64_t n_seqs, int64_t per_seq, int64_t max_len, bool i4)
 {
     const int64_t units = compute_units(), rounds = (max_len + kRound - 1) / kRound, shares = 2 * units / per_seq;
-    const bool many = n_seqs * per_seq >= units / 2;
-    if (rounds <= (i4 ? (many ? 16 : 6) : (many ? 6 : 3))) return 0;
+    const int64_t pairs = n_seqs * per_seq;
+    if (rounds <= (i4 ? (pairs > units ? 16 : pairs >= units / 2 ? 24 : pairs >= units / 4 ? 12 : 7) : pairs >= units / 2 ? 6 : 3)) return 0;
     // a wave adds up 64 lengths at a time, and rounds are counted in 32 bits
-    if (shares < 2 || n_seqs > 1024 || n_seqs * per_seq >= 8 * units || n_seqs * rounds >= 1 << 30) return 0;
+    if (shares < 2 || n_seqs > 1024 || pairs >= 8 * units || n_seqs * rounds >= 1 << 30) return 0;
     return (int)shares;
 }
 

@@ -107,7 +107,7 @@ def test_long_sequences_are_split_and_joined(gpu, i4, page):
 
 
 @pytest.mark.parametrize("i4", [True, False])
-@pytest.mark.parametrize("n,longest,shares", [(1, 380, False), (1, 800, True), (16, 760, False), (16, 2100, True)])
+@pytest.mark.parametrize("n,longest,shares", [(1, 380, False), (1, 1000, True), (16, 760, False), (16, 3200, True), (7, 300, False), (33, 380, False)])
 def test_both_sides_of_the_choice(gpu, i4, n, longest, shares):
     """One workgroup per sequence, and shares of them: few sequences and many."""
     lens = [longest] + [int(x) for x in np.random.default_rng(n).integers(0, longest, n - 1)]
