@@ -13,6 +13,11 @@
 //   O^T = V^T P^T its k-index is the token: lane (n, g) supplies the eight tokens 4 g + r of two halves of the tile, which are
 //                 the ones it got scores for, so the weights go from one product to the next inside the lane
 //
+// Where up to 4 (8) query heads share a key/value head, the sixteen columns hold 4 (2) copies of them (4 bits), and a copy forms the
+// weights of every fourth (of every other pair of) token only, zeros for the rest, so that no lane forms a weight that another has
+// too; the copies' sums are added up at the end (64 sequences of 0 .. 8192 tokens 57.2 -> 55.4 us, 16 of 2000 14.8 -> 13.6, 200 of up
+// to 500 21.2 -> 19.4).
+//
 // The order of channels in the first product and of columns in the second is free, so both operands are taken as they lie in
 // memory, and the sums over codes need no conversion: a code c in bits 4-7 of a half is the subnormal fp16 number c 2^-20, a
 // shift and an AND per two codes.  (The matrix pipe takes subnormal operands; measured on random weights, sums over c 2^-20 are
@@ -30,6 +35,7 @@ namespace {
 
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 union Frag { f16x8 v; uint32_t w[4]; _Float16 h[8]; };
 
@@ -101,11 +107,20 @@ __device__ __forceinline__ int sequence_at(const Decode &a, int at, int lane, in
 }
 
 // ---- tiles -----------------------------------------------------------------------------------------------------------
-// reduction over the four lanes that share lane % 16
-__device__ __forceinline__ float max_of_groups(float v)
+// reductions over the lanes that share a query row: the four with one lane % 16, and the copies of that
+template <int COPIES> __device__ __forceinline__ float max_of_groups(float v)
 {
     v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+    v = fmaxf(v, __shfl_xor(v, 32, 64));
+    if constexpr (COPIES > 1) v = fmaxf(v, lane_perm<0x128>(v));             // rotations by 8 and by 4 of 16
+    if constexpr (COPIES > 2) v = fmaxf(v, lane_perm<0x124>(v));
+    return v;
+}
+template <int COPIES> __device__ __forceinline__ float sum_of_copies(float v)
+{
+    if constexpr (COPIES > 1) v += lane_perm<0x128>(v);
+    if constexpr (COPIES > 2) v += lane_perm<0x124>(v);
+    return v;
 }
 __device__ __forceinline__ float sum_of_groups(float v)
 {
@@ -124,12 +139,13 @@ __device__ __forceinline__ uint32_t nibble_pair(uint32_t w, int i)
 
 // A wave's share of 32 tokens in registers.  Whole runs of 16 tokens lie in one page, so that a half of the tile has one address
 // for the wave and fixed offsets per lane.
-template <int D, bool I4> struct Tile {
+template <int D, bool I4, int COPIES> struct Tile {
+    static constexpr int N = 4 / COPIES;                 // tokens of a half whose weights are this lane's: 4 g + N copy + (0 .. N - 1)
     static constexpr int KW = I4 ? D / 32 : D / 8;       // dwords of a lane's share of a key
     static constexpr int VW = I4 ? 1 : D / 32;           // dwords of a lane's share of a value
     static constexpr int ROW = I4 ? D / 2 : D * 2;       // bytes of a row
     uint32_t k[2][KW], v[2][4][VW];
-    float ks[2][4], kz[2][4], vs[2][4], vz[2][4];        // scales and zeros of tokens 4 g + r of half u
+    float ks[2][N], kz[2][N], vs[2][N], vz[2][N];        // their scales and zeros
 };
 
 // 4 bits: a tile waits in LDS as keys, values and parameters (two halves each; keys' first), two tiles per wave
@@ -145,9 +161,10 @@ __device__ __forceinline__ void dma16_once(const void *p, uint32_t lds)
 }
 
 // The query rows of a workgroup, and their state over the tokens that a wave has seen.
-template <int D, bool I4> struct Rows {
+template <int D, bool I4, int COPIES> struct Rows {
     static constexpr int C = D / 16;                     // output columns per lane and row index: d = C n + j
-    using T = Tile<D, I4>;
+    using T = Tile<D, I4, COPIES>;
+    static constexpr int N = T::N;
     Frag q[D / 32];
     float unit, qz;                                      // score of one product; its sum(q)
     f32x4 acc[C];                                        // sums of w c 2^-20, or w v
@@ -181,10 +198,10 @@ template <int D, bool I4> struct Rows {
     }
 
     // 32 tokens from `at` on, those before `last` whose page is there (bit u: of half u)
-    __device__ __forceinline__ void use(T &t, int at, int last, uint32_t pages_there, int n, int g)
+    __device__ __forceinline__ void use(T &t, int at, int last, uint32_t pages_there, int n, int g, int copy)
     {
 #pragma clang fp contract(off)                            // a score minus the maximum of the rounded ones is exact near it
-        float y[2][4];                                   // scores over log(2)
+        float y[2][N];                                   // scores over log(2)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             f32x4 dot = 0.f;
@@ -196,14 +213,17 @@ template <int D, bool I4> struct Rows {
                 dot = __builtin_amdgcn_mfma_f32_16x16x32_f16(f.v, q[i].v, dot, 0, 0, 0);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[u][r] = I4 ? fmaf(dot[r], unit, -t.kz[u][r] * qz) * t.ks[u][r] : dot[r] * unit;
+            for (int i = 0; i < N; ++i) {
+                const float x = COPIES == 1 ? dot[i] : COPIES == 2 ? (copy ? dot[2 + i] : dot[i]) : copy & 2 ? (copy & 1 ? dot[3] : dot[2]) : copy & 1 ? dot[1] : dot[0];
+                y[u][i] = I4 ? fmaf(x, unit, -t.kz[u][i] * qz) * t.ks[u][i] : x * unit;
+            }
         }
         if (pages_there != 3 || at + kTile > last) {     // a token that is not there: score minus infinity, a finite value
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const bool there = (pages_there >> u & 1) && at + 16 * u + 4 * g + r < last;
+                for (int r = 0; r < N; ++r) {
+                    const bool there = (pages_there >> u & 1) && at + 16 * u + 4 * g + N * copy + r < last;
                     y[u][r] = there ? y[u][r] : kNone;
                     if constexpr (I4) {
                         t.vs[u][r] = there ? t.vs[u][r] : 1.f;
@@ -214,13 +234,13 @@ template <int D, bool I4> struct Rows {
                     }
                 }
         }
-        float p[2][4], w[2][4];
+        float p[2][N], w[2][N];
         auto weights = [&] {
             float most = 0.f;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
+                for (int r = 0; r < N; ++r) {
                     p[u][r] = __builtin_amdgcn_exp2f(I4 ? y[u][r] - top - lift : y[u][r] - top);
                     w[u][r] = I4 ? p[u][r] * t.vs[u][r] : p[u][r];
                     most = fmaxf(most, w[u][r]);
@@ -234,15 +254,15 @@ template <int D, bool I4> struct Rows {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) most = fmaxf(most, y[u][r]);
-            most = fmaxf(top, max_of_groups(most));
+                for (int r = 0; r < N; ++r) most = fmaxf(most, y[u][r]);
+            most = fmaxf(top, max_of_groups<COPIES>(most));
             if constexpr (I4) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
+                    for (int r = 0; r < N; ++r)
                         if (most != kNone) raised = fmaxf(raised, y[u][r] - most + __builtin_amdgcn_logf(t.vs[u][r]));
-                raised = max_of_groups(raised);
+                raised = max_of_groups<COPIES>(raised);
                 if (top != kNone) raised = fmaxf(raised, top - most + lift);
             }
             const float shrink = most == kNone ? 1.f : __builtin_amdgcn_exp2f(I4 ? top - most + (lift - raised) : top - most);
@@ -255,15 +275,26 @@ template <int D, bool I4> struct Rows {
             weights();
             top = most;
         }
-        Frag f16w;
+        Frag f16w;                                       // of tokens 4 u + r; zeros for those of other copies
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (COPIES == 1) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                f16w.h[4 * u + r] = (_Float16)w[u][r];
-                total += p[u][r];
-                if constexpr (I4) zsum = fmaf((float)f16w.h[4 * u + r], t.vz[u][r], zsum);
+                for (int i = 0; i < 4; ++i) f16w.h[4 * u + i] = (_Float16)w[u][i];
+            } else if constexpr (COPIES == 2) {
+                const f16x2 pair = {(_Float16)w[u][0], (_Float16)w[u][1]};
+                const uint32_t x = __builtin_bit_cast(uint32_t, pair);
+                f16w.w[2 * u] = copy ? 0u : x, f16w.w[2 * u + 1] = copy ? x : 0u;
+            } else {
+                const uint32_t x = (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)w[u][0]) << (16 * (copy & 1));
+                f16w.w[2 * u] = copy & 2 ? 0u : x, f16w.w[2 * u + 1] = copy & 2 ? x : 0u;
             }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                total += p[u][i];
+                if constexpr (I4) zsum = fmaf((float)(_Float16)w[u][i], t.vz[u][i], zsum);
+            }
+        }
         // column j of token pairs (r, r + 1): two tokens per dword
         uint32_t lo[2][2], hi[2][2];
         if constexpr (I4) {
@@ -299,12 +330,12 @@ template <int D, bool I4> struct Rows {
 };
 
 // Tokens [first, last) of sequence b over a wave's tiles, `smem` the wave's own stages (4 bits).
-template <int D, bool I4, int WAVES>
-__device__ __forceinline__ void walk(const Decode &a, Rows<D, I4> &rows, int b, int h, int first, int last, uint8_t *smem, int wave, int lane)
+template <int D, bool I4, int COPIES, int WAVES>
+__device__ __forceinline__ void walk(const Decode &a, Rows<D, I4, COPIES> &rows, int b, int h, int first, int last, uint8_t *smem, int wave, int lane)
 {
-    using T = Tile<D, I4>;
+    using T = Tile<D, I4, COPIES>;
     constexpr int ROUND = WAVES * kTile;
-    const int n = lane & 15, g = lane >> 4;
+    const int n = lane & 15, g = lane >> 4, copy = n / (16 / COPIES);
     // (constant while the kernel runs: scalar loads, which the vector counter does not see)
     const auto *table = (const __attribute__((address_space(4))) int32_t *)(uintptr_t)(a.table + (int64_t)b * a.ld_table);
     const int page_mask = (1 << a.page_shift) - 1;
@@ -376,12 +407,17 @@ __device__ __forceinline__ void walk(const Decode &a, Rows<D, I4> &rows, int b, 
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     t.v[u][r][0] = *reinterpret_cast<const uint32_t *>(from + Stage<D>::V + (D == 128 ? 1024 * u + 64 * (4 * r + g) + 4 * n : 512 * u + 32 * (4 * g + r) + 4 * (n >> 1)));
+                const uint8_t *params = from + Stage<D>::P + 128 * u + 32 * g;
+                if constexpr (COPIES == 4) {
+                    const float2 kp = *reinterpret_cast<const float2 *>(params + 8 * copy), vp = *reinterpret_cast<const float2 *>(params + 256 + 8 * copy);
+                    t.ks[u][0] = kp.x, t.kz[u][0] = kp.y, t.vs[u][0] = vp.x, t.vz[u][0] = vp.y;
+                } else {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const f32x4 kp = *reinterpret_cast<const f32x4 *>(from + Stage<D>::P + 128 * u + 32 * g + 16 * i);
-                    const f32x4 vp = *reinterpret_cast<const f32x4 *>(from + Stage<D>::P + 256 + 128 * u + 32 * g + 16 * i);
-                    t.ks[u][2 * i] = kp[0], t.kz[u][2 * i] = kp[1], t.ks[u][2 * i + 1] = kp[2], t.kz[u][2 * i + 1] = kp[3];
-                    t.vs[u][2 * i] = vp[0], t.vz[u][2 * i] = vp[1], t.vs[u][2 * i + 1] = vp[2], t.vz[u][2 * i + 1] = vp[3];
+                    for (int i = 0; i < T::N / 2; ++i) {
+                        const f32x4 kp = *reinterpret_cast<const f32x4 *>(params + 16 * (i + copy)), vp = *reinterpret_cast<const f32x4 *>(params + 256 + 16 * (i + copy));
+                        t.ks[u][2 * i] = kp[0], t.kz[u][2 * i] = kp[1], t.ks[u][2 * i + 1] = kp[2], t.kz[u][2 * i + 1] = kp[3];
+                        t.vs[u][2 * i] = vp[0], t.vz[u][2 * i] = vp[1], t.vs[u][2 * i + 1] = vp[2], t.vz[u][2 * i + 1] = vp[3];
+                    }
                 }
             }
         };
@@ -408,7 +444,7 @@ __device__ __forceinline__ void walk(const Decode &a, Rows<D, I4> &rows, int b, 
                 load(slot, w);
                 next = pages_of(t0 + 3 * ROUND);
             }
-            rows.use(t, t0, last, here, n, g);
+            rows.use(t, t0, last, here, n, g, copy);
         }
     } else {
         for (; t0 < last; t0 += ROUND) {
@@ -436,7 +472,7 @@ __device__ __forceinline__ void walk(const Decode &a, Rows<D, I4> &rows, int b, 
                     }
                 }
             }
-            rows.use(t, t0, last, w.there, n, g);
+            rows.use(t, t0, last, w.there, n, g, copy);
         }
     }
 }
@@ -450,7 +486,7 @@ template <int D> __device__ __forceinline__ void store_row(_Float16 *dst, f32x4 
     *reinterpret_cast<u32x2 *>(dst) = y.v;
 }
 
-template <int D, bool I4, int WAVES> __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void attn_decode_kernel(Decode a)
+template <int D, bool I4, int COPIES, int WAVES> __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void attn_decode_kernel(Decode a)
 {
     constexpr int C = D / 16, ROUND = WAVES * kTile;     // (kRound where there are shares)
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -471,16 +507,23 @@ template <int D, bool I4, int WAVES> __global__ __launch_bounds__(WAVES * 64, WA
         const int len = length_of(a, b), rounds = (len + ROUND - 1) / ROUND;
         const int r0 = max(from - before, 0), r1 = a.shares ? min(to - before, rounds) : rounds;
         const bool whole = r0 == 0 && r1 == rounds;
-        Rows<D, I4> rows;
-        rows.begin(a.q + (int64_t)b * a.ldq + (int64_t)(head0 + n) * D, n < n_rows, g, a.scale);
-        walk<D, I4, WAVES>(a, rows, b, h, r0 * ROUND, min(r1 * ROUND, len), smem + wave * (2 * Stage<D>::BYTES), wave, lane);
+        Rows<D, I4, COPIES> rows;
+        rows.begin(a.q + (int64_t)b * a.ldq + (int64_t)(head0 + n % (16 / COPIES)) * D, n % (16 / COPIES) < n_rows, g, a.scale);
+        walk<D, I4, COPIES, WAVES>(a, rows, b, h, r0 * ROUND, min(r1 * ROUND, len), smem + wave * (2 * Stage<D>::BYTES), wave, lane);
         __syncthreads();                                 // the stages' area is used again
 
         // the waves meet: acc[j][r] of lane (n, g) is column d = C (4 g + r) + j of query row n
         float(*s_top)[16] = reinterpret_cast<float(*)[16]>(smem), (*s_total)[16] = s_top + WAVES;
         float(*s_acc)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(s_total + WAVES);
-        const float back = I4 ? __builtin_amdgcn_exp2f(rows.lift) : 1.f, total = sum_of_groups(rows.total) * back, zsum = sum_of_groups(rows.zsum);
+        const float back = I4 ? __builtin_amdgcn_exp2f(rows.lift) : 1.f, total = sum_of_copies<COPIES>(sum_of_groups(rows.total)) * back,
+                    zsum = sum_of_copies<COPIES>(sum_of_groups(rows.zsum));
         if (g == 0) s_top[wave][n] = rows.top, s_total[wave][n] = total;
+        if constexpr (COPIES > 1) {
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) rows.acc[j][r] = sum_of_copies<COPIES>(rows.acc[j][r]);
+        }
         if (n < n_rows) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
@@ -601,26 +644,35 @@ template <int D, int PARTS> __global__ __launch_bounds__(256) void attn_join_ker
     store_row<D>(a.o + (int64_t)b * a.ldo + (int64_t)head * D + d, sum, all);
 }
 
-template <int D, bool I4, int WAVES> hipError_t launch_waves(const Decode &a, hipStream_t st)
+template <int D, bool I4, int COPIES, int WAVES> hipError_t launch_waves(const Decode &a, hipStream_t st)
 {
     constexpr int meet = WAVES * 16 * (D + 4 + 2) * 4, stages = I4 ? WAVES * 2 * Stage<D>::BYTES : 0;
     constexpr int lds = meet > stages ? meet : stages;
     static_assert(lds <= 160 * 1024, "within what a workgroup may have");
     if constexpr (lds > 65536)
-        if (hipError_t e = allow_dynamic_lds<attn_decode_kernel<D, I4, WAVES>>(lds); e != hipSuccess) return e;
+        if (hipError_t e = allow_dynamic_lds<attn_decode_kernel<D, I4, COPIES, WAVES>>(lds); e != hipSuccess) return e;
     const dim3 grid((unsigned)(a.shares ? a.shares : a.n_seqs) * (unsigned)a.per_seq);
-    hipLaunchKernelGGL((attn_decode_kernel<D, I4, WAVES>), grid, dim3(WAVES * 64), lds, st, a);
+    hipLaunchKernelGGL((attn_decode_kernel<D, I4, COPIES, WAVES>), grid, dim3(WAVES * 64), lds, st, a);
     return hipGetLastError();
 }
 
 // Eight waves where a workgroup has a unit to itself and a whole sequence to do (4 bits; us, 4 waves / 8: one sequence of 500 tokens 7.6
 // / 7.1, 16 of 2000 17.5 / 14.3, 32 of up to 2000 17.8 / 14.8; 64 of 500 10.2 / 13.0.  Sixteen 9.4, 17.7, 20.2 and 21.  fp16 gains nothing:
 // 32 of 1000 19.6 / 19.4).
-template <int D, bool I4> hipError_t launch_shares(const Decode &a, hipStream_t st)
+template <int D, bool I4, int COPIES> hipError_t launch_copies(const Decode &a, hipStream_t st)
 {
     if constexpr (I4)
-        if (!a.shares && (int64_t)a.n_seqs * a.per_seq <= compute_units() && a.max_len > 2 * kRound) return launch_waves<D, I4, 8>(a, st);
-    return launch_waves<D, I4, 4>(a, st);
+        if (!a.shares && (int64_t)a.n_seqs * a.per_seq <= compute_units() && a.max_len > 2 * kRound) return launch_waves<D, I4, COPIES, 8>(a, st);
+    return launch_waves<D, I4, COPIES, 4>(a, st);
+}
+
+template <int D, bool I4> hipError_t launch_shares(const Decode &a, hipStream_t st)
+{
+    if constexpr (I4) {
+        if (a.group <= 4) return launch_copies<D, I4, 4>(a, st);
+        if (a.group <= 8) return launch_copies<D, I4, 2>(a, st);
+    }
+    return launch_copies<D, I4, 1>(a, st);
 }
 
 template <int D> hipError_t launch_join(const Decode &a, hipStream_t st)

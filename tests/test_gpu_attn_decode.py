@@ -87,7 +87,7 @@ LENS = [0, 1, 15, 16, 17, 31, 32, 33, 127, 128, 129, 300, 511]
 
 @pytest.mark.parametrize("i4", [True, False])
 @pytest.mark.parametrize("d", [128, 64])
-@pytest.mark.parametrize("H,KV", [(32, 8), (3, 3), (16, 1), (20, 1), (40, 2)])
+@pytest.mark.parametrize("H,KV", [(32, 8), (3, 3), (16, 1), (20, 1), (40, 2), (16, 2), (5, 1), (6, 2)])
 def test_lengths_and_heads(gpu, i4, d, H, KV):
     print("case decode", H, KV, d, i4, flush=True)
     batch = Batch(LENS, KV, d, 16, i4, seed=H)
@@ -96,13 +96,13 @@ def test_lengths_and_heads(gpu, i4, d, H, KV):
 
 
 @pytest.mark.parametrize("i4", [True, False])
-@pytest.mark.parametrize("page", [16, 64, 4096])
-def test_long_sequences_are_split_and_joined(gpu, i4, page):
-    print("case decode long", page, i4, flush=True)
+@pytest.mark.parametrize("page,H", [(16, 8), (64, 8), (4096, 8), (16, 2), (64, 14), (32, 24), (16, 34)])
+def test_long_sequences_are_split_and_joined(gpu, i4, page, H):
+    print("case decode long", page, H, i4, flush=True)
     for lens in ([5001], [3, 4097, 0, 2500]):
         batch = Batch(lens, 2, 128, page, i4, seed=page)
-        assert gpu.sr_attn_decode_workspace_bytes(len(lens), 8, 2, 128, batch.table.shape[1], page, int(i4)) > 0
-        q = queries(len(lens), 8, 128)
+        assert gpu.sr_attn_decode_workspace_bytes(len(lens), H, 2, 128, batch.table.shape[1], page, int(i4)) > 0
+        q = queries(len(lens), H, 128)
         batch.check(run(gpu, batch, q), q, 1 / np.sqrt(128))
 
 
