@@ -48,6 +48,8 @@ union Frag { f16x8 v; s16x4 s[2]; f16x2 p[4]; };
 
 constexpr int kMatrix = 0x8, kRead = 0x100;              // groups of instructions for the scheduler: matrix products, reads from LDS
 constexpr float kNone = -__builtin_inff();
+// Workgroups of one row of the grid: a launch of 2^32 and more work items along one dimension is not refused, it wraps.
+constexpr int kGridShift = 22;
 
 struct Prefill {
     const _Float16 *q, *k, *v;
@@ -117,6 +119,7 @@ __device__ __forceinline__ bool find_tile(const Prefill &a, int tile, int lane, 
         return true;
     }
     tile = a.tiles - 1 - tile;
+    if (tile < 0) return false;                          // (a workgroup that only rounds the grid up)
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
         const int s = min(s0 + lane, a.n_seqs - 1);
         const int q_from = a.cu_q[s], q_to = a.cu_q[s + 1], k_from = a.cu_k[s], k_to = a.cu_k[s + 1];
@@ -149,11 +152,11 @@ template <int D, int W, int SETS, int KEYS> __global__ __launch_bounds__(64 * W 
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem + set * 4 * kTileBytes;
     const uint8_t *tiles = smem + set * 4 * kTileBytes;
     // neighbouring workgroups take different key/value heads: an XCD, every eighth of them, keeps few heads' keys in its L2
-    const uint32_t blocks = (uint32_t)a.heads >> a.head_shift, x = blockIdx.x % blocks;
+    const uint32_t blocks = (uint32_t)a.heads >> a.head_shift, number = (blockIdx.y << kGridShift) + blockIdx.x, x = number % blocks;
     const int kvh = (int)(x % (uint32_t)a.kv);
     const int head = kvh * a.group + ((int)(x / (uint32_t)a.kv) << a.head_shift) + (wave & ((1 << a.head_shift) - 1));
     Place p;
-    if (!find_tile(a, (int)(blockIdx.x / blocks), lane, p)) return;
+    if (!find_tile(a, (int)(number / blocks), lane, p)) return;
     const int rows = 1 << a.row_shift, r0 = p.local << a.row_shift, shift = p.nk - p.nq;
     const int end = a.causal ? min(p.nk, min(r0 + rows, p.nq) + shift) : p.nk;         // keys that any row sees
     const int w0 = r0 + 32 * (wave >> a.head_shift), row = w0 + m;
@@ -413,7 +416,9 @@ template <int D, int W, int SETS, int KEYS> hipError_t launch_dim(Prefill a, int
     const int64_t blocks = a.heads >> a.head_shift;
     a.tiles = (int)tiles_of(a.tokens_q, n_seqs, 1 << a.row_shift);
     a.at_once = balance ? (int)((compute_units() + blocks - 1) / blocks) : 0;
-    hipLaunchKernelGGL((attn_prefill_kernel<D, W, SETS, KEYS>), dim3((unsigned)(a.tiles * blocks)), dim3(64 * W * SETS), bytes, st, a);
+    static_assert((64ll * W * SETS << kGridShift) < 1ll << 32, "a row of the grid");
+    const int64_t all = a.tiles * blocks, row = std::min(all, (int64_t)1 << kGridShift);
+    hipLaunchKernelGGL((attn_prefill_kernel<D, W, SETS, KEYS>), dim3((unsigned)row, (unsigned)((all + row - 1) / row)), dim3(64 * W * SETS), bytes, st, a);
     return hipGetLastError();
 }
 
