@@ -54,7 +54,7 @@ typedef struct {
  *                  rows of a batch).  Slots that occur twice leave that slot's contents unspecified.
  *   cos_sin        fp32 [max_pos, head_dim]: cosines, then sines, of a position's head_dim / 2 angles; NULL: no rotation
  *                  (positions may then be NULL).  max_pos < 2^31.
- *   clip           in (0, 1] (paper: 0.95; SR_KV_I4 only)
+ *   clip           in [2^-64, 1] (paper: 0.95; SR_KV_I4 only)
  *   Q_out          fp16 [T, n_heads * head_dim], row stride ldqo: the turned queries.  May be Q_f16 (same stride).
  *   K_out          NULL, or fp16 [T, n_kv_heads * head_dim], row stride ldko: the turned keys before quantisation.  May be
  *                  K_f16 (same stride).

@@ -128,21 +128,23 @@ template <int D> __device__ __forceinline__ uint32_t quantise_row(const Eight &x
     const float hi = clip * mx, lo = clip * mn;
     scale = hi == lo ? 1.f : (hi - lo) * (1.f / 15.f);
     // Quotients from the correctly rounded reciprocal y: q = a y, and one step q + (a - q d) y with the exact remainder gives
-    // the correctly rounded a / d (Markstein, 1990); a and d are far from the ends of fp32's range.
+    // the correctly rounded a / d (Markstein, 1990); a and d are far from the ends of fp32's range (d is 2^-92 at least).
     const float y = 1.f / scale;
     auto over_scale = [&](float a) {
         const float q = a * y;
         return fmaf(fmaf(-q, scale, a), y, q);
     };
     zero = -rintf(over_scale(lo));
-    // Adding 1.5 * 2^23 rounds a quotient (below 2^16 in size) to the nearest integer, ties to even, in the low bits.
+    // clamp(rint(q) + z, 0, 15) = rint(clamp(q, -z, 15 - z)) + z: |z| is below 2^16 whatever the clipping ratio (a row's range is at
+    // least one fp16 spacing of its largest value), while q grows with the ratio's inverse.  Adding 1.5 * 2^23 rounds the clamped
+    // quotient to the nearest integer, ties to even, in the low bits.
     constexpr uint32_t kMagic = 0x4B400000u;
     const int shift = (int)zero - (int)kMagic;
     uint32_t word = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int c = (int)__float_as_uint(over_scale(v[e]) + __uint_as_float(kMagic)) + shift;
-        word |= (uint32_t)min(max(c, 0), 15) << (4 * e);
+        const float q = __builtin_amdgcn_fmed3f(over_scale(v[e]), -zero, 15.f - zero);
+        word |= (uint32_t)((int)__float_as_uint(q + __uint_as_float(kMagic)) + shift) << (4 * e);
     }
     return word;
 }

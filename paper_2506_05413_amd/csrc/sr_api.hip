@@ -318,6 +318,7 @@ int sr_kv_quant_asym(const void *X_f16, int64_t rows, int64_t D, int64_t ldx, in
 static bool head_dim_ok(int64_t d) { return d == 64 || d == 128; }
 
 static constexpr int64_t kMostHeads = 1 << 16;             // kernels divide rows by heads in fp32
+static constexpr float kLeastClip = 0x1p-64f;              // steps and their reciprocals stay normal numbers
 static int check_cache(const sr_kv_cache *cache, sr::KvCache &c)
 {
     if (!cache) return SR_ERR_NULL;
@@ -352,7 +353,7 @@ int sr_rope_kv_append(const void *Q_f16, int64_t ldq, const void *K_f16, int64_t
     if (T < 0 || n_heads < 0 || n_heads >= kMostHeads || ldk < dk || ldv < dk || (n_heads && (ldq < dq || ldqo < dq)) || (K_out && ldko < dk))
         return SR_ERR_SHAPE;
     if (T >= (1 << 27) || T * (n_heads + 2 * c.heads) >= (1 << 27)) return SR_ERR_SHAPE;
-    if (flags & ~(SR_ROPE_PAIRS | SR_ROPE_HADAMARD) || (c.i4 && !(clip > 0.f && clip <= 1.f))) return SR_ERR_ARG;
+    if (flags & ~(SR_ROPE_PAIRS | SR_ROPE_HADAMARD) || (c.i4 && !(clip >= kLeastClip && clip <= 1.f))) return SR_ERR_ARG;
     if (cos_sin && (max_pos < 1 || max_pos >= ((int64_t)1 << 31))) return SR_ERR_SHAPE;
     if (T == 0) return SR_OK;
     if (!K_f16 || !V_f16 || !slots || (cos_sin && !positions) || (n_heads && (!Q_f16 || !Q_out))) return SR_ERR_NULL;
