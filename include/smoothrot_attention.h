@@ -26,8 +26,9 @@ enum { SR_KV_F16 = 0, SR_KV_I4 = 1 };
  * The cache: pages of page_size tokens, each page one head after the other.  Token i of a page is "slot" page * page_size + i.
  *   K, V                SR_KV_F16: fp16 [n_pages][n_kv_heads][page_size][head_dim]
  *                       SR_KV_I4:  uint8 [n_pages][n_kv_heads][page_size][head_dim / 2], packed like sr_kv_quant_asym's Q
- *   K_params, V_params  SR_KV_I4: fp32 [n_pages][n_kv_heads][page_size][2] (d, z): value = (code - z) * d, d > 0, both finite.
- *                       NULL for SR_KV_F16.
+ *   K_params, V_params  SR_KV_I4: fp32 [n_pages][n_kv_heads][page_size][2] (d, z): value = (code - z) * d, of the size of fp16
+ *                       numbers, d > 0, |z| < 2^24; d = NaN for a row of NaN, which reaches the query heads that read it, in
+ *                       its own sequence.  NULL for SR_KV_F16.
  * page_size a power of two, 16 <= page_size <= 2^20 (SR_ERR_ARG otherwise), n_pages >= 1, n_pages * page_size < 2^40.
  * The struct lies in host memory and is read during the call only.  Slots that no sequence holds may contain anything.
  */
@@ -46,7 +47,8 @@ typedef struct {
  *                                                     alike, which leaves q . k what it was (paper: head-wise online Hadamard)
  * in fp32 (every operation rounded), then rounded to fp16.  Values are not turned.  A 4-bit cache receives the codes of those
  * fp16 numbers under the formula of sr_kv_quant_asym with group = head_dim, d = (hi - lo) times the fp32 number nearest 1 / 15,
- * quotients by d correctly rounded (so d may differ from sr_kv_quant_asym's by a rounding, and a code on a rounding boundary).
+ * quotients by d correctly rounded (so d may differ from sr_kv_quant_asym's by a rounding, and a code on a rounding boundary).  A row
+ * (one head of one token) with a NaN or an infinity, the transform's own overflow included, gets d = NaN, and so stands for NaN.
  *   Q_f16          fp16 [T, n_heads * head_dim], row stride ldq; may be NULL with n_heads = 0
  *   K_f16, V_f16   fp16 [T, n_kv_heads * head_dim], row strides ldk, ldv (e.g. columns of one fused projection)
  *   positions      int32 [T]; positions outside [0, max_pos) are taken as the nearest inside

@@ -112,10 +112,29 @@ template <int D, bool PAIRS> __device__ __forceinline__ void rotate_row(float (&
     }
 }
 
-// four-bit codes of a row spread over D / 8 lanes; scale and zero are the same in all of them
-template <int D> __device__ __forceinline__ uint32_t quantise_row(const Eight &x, float clip, float &scale, float &zero)
+// NaN if one of eight numbers is infinite or none, else zero
+__device__ __forceinline__ float not_finite(const Eight &x)
+{
+    const f16x2 none = {(_Float16)0.f, (_Float16)0.f};
+    f16x2 t = x.p[0] * none;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) t = __builtin_elementwise_fma(x.p[i], none, t);
+    return (float)(t[0] + t[1]);
+}
+
+// Four-bit codes of a row spread over D / 8 lanes; scale and zero are the same in all of them.  A row with a value that is not finite
+// (a key may become so by the transform) has no codes: it gets those of zeros, and NaN for its scale.
+template <int D> __device__ __forceinline__ uint32_t quantise_row(Eight x, float clip, float &scale, float &zero)
 {
 #pragma clang fp contract(off)
+    float bad = not_finite(x);
+    if (__any(bad != bad)) {                                                     // (seldom: the maximum below takes no notice of NaN)
+        bad += lane_perm<0xB1>(bad);
+        bad += lane_perm<0x4E>(bad);
+        bad += lane_perm<0x141>(bad);
+        if constexpr (D == 128) bad += lane_perm<0x140>(bad);
+        if (bad != bad) x.v = 0u;
+    }
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = __half2float(x.h[e]);
@@ -146,6 +165,7 @@ template <int D> __device__ __forceinline__ uint32_t quantise_row(const Eight &x
         const float q = __builtin_amdgcn_fmed3f(over_scale(v[e]), -zero, 15.f - zero);
         word |= (uint32_t)((int)__float_as_uint(q + __uint_as_float(kMagic)) + shift) << (4 * e);
     }
+    scale += bad;
     return word;
 }
 
