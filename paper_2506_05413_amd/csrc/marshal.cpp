@@ -387,7 +387,8 @@ PyObject *rope_kv_append(PyObject *const *a)
     int64_t max_pos = 0;
     if (a[5] != Py_None) {
         const at::Tensor &t = here(matrix(a[5], at::kFloat, "cos_sin"), "cos_sin");
-        if (t.size(1) != c.head_dim || !t.is_contiguous()) value_error("%s has the wrong shape", "cos_sin");
+        // (one without a row has no address, which would read as "no rotation")
+        if (t.size(0) < 1 || t.size(1) != c.head_dim || !t.is_contiguous()) value_error("%s has the wrong shape", "cos_sin");
         table = floats(t), max_pos = t.size(0);
         positions = at_of<int32_t>(indices(a[3], "positions", at::kInt, T));
     }

@@ -1,5 +1,5 @@
 """sr_rope_kv_append where the quantiser's numbers leave the ordinary: clipping ratios far below 1, rows that hold a NaN or an
-infinity, or reach one."""
+infinity, or reach one; and tables of angles without a row."""
 import numpy as np
 import pytest
 import torch
@@ -116,3 +116,14 @@ def test_a_16_bit_cache_takes_rows_as_they_are(gpu):
     torch.cuda.synchronize()
     np.testing.assert_array_equal(gk.cpu().numpy().reshape(k.shape), k)
     np.testing.assert_array_equal(gv.cpu().numpy().reshape(v.shape), v)
+
+
+def test_a_table_without_a_row_is_refused(gpu):
+    """It has no address, which must not read as "no rotation"."""
+    x = torch.ones((3, 64), dtype=torch.float16, device="cuda")
+    at = torch.zeros(3, dtype=torch.int32, device="cuda")
+    cache = make_cache(1, 1, 16, 64, False)
+    with pytest.raises(ValueError):
+        gpu.sr_rope_kv_append(x, x, x, at, at.long(), torch.empty((0, 64), device="cuda"), cache)
+    torch.cuda.synchronize()
+    assert torch.isnan(cache[0]).all()
