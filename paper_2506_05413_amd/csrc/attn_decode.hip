@@ -486,7 +486,7 @@ template <int D> __device__ __forceinline__ void store_row(_Float16 *dst, f32x4 
     *reinterpret_cast<u32x2 *>(dst) = y.v;
 }
 
-template <int D, bool I4, int COPIES, int WAVES> __global__ __launch_bounds__(WAVES * 64, WAVES == 16 ? 4 : 2) void attn_decode_kernel(Decode a)
+template <int D, bool I4, int COPIES, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void attn_decode_kernel(Decode a)
 {
     constexpr int C = D / 16, ROUND = WAVES * kTile;     // (kRound where there are shares)
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];

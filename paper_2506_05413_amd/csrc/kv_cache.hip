@@ -24,13 +24,11 @@ union Eight { u32x4 v; uint32_t w[4]; __half h[8]; f16x2 p[4]; };
 // Lane l of a row holds the eight values number l ^ 3 if bit 2 of l is set, else l: number ^ 4 then is in lane l ^ 7, which is one
 // exchange (l ^ 4 would be two).  Everything below goes by that number, called lane.
 __device__ __forceinline__ int number_of(int l) { return l ^ (l & 4 ? 3 : 0); }
-// number ^ MASK inside a row of 16 lanes
-template <int MASK, typename T> __device__ __forceinline__ T lane_xor(T v)
+// number ^ MASK inside a row of 16 lanes, MASK half of a row of D / 8
+template <int MASK> __device__ __forceinline__ int lane_xor(int v)
 {
-    if constexpr (MASK == 1) return lane_perm<0xB1>(v);
-    else if constexpr (MASK == 2) return lane_perm<0x4E>(v);
-    else if constexpr (MASK == 4) return lane_perm<0x141>(v);                     // lane 7 - l of eight
-    else return lane_perm<0x128>(v);                                              // rotation by 8 of 16
+    static_assert(MASK == 4 || MASK == 8);
+    return lane_perm<MASK == 4 ? 0x141 : 0x128>(v);                               // lane 7 - l of eight; rotation by 8 of 16
 }
 
 // Lanes with bit MASK clear get own + other, the others own - other, the negative of what the transform says: one fused
