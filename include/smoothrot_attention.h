@@ -114,7 +114,7 @@ SR_API int sr_attn_decode(const void *Q_f16, int64_t ldq, int64_t n_seqs, int64_
  *                  cut to [0, T_q] and [0, T_k]).  Rows of no sequence are left as they were.
  *   scale          0 < scale <= 2^64
  *   O_f16          out, fp16 [T_q, n_heads * head_dim], row stride ldo.  May be Q_f16 (same stride).
- * T_q, T_k < 2^31, row strides < 2^23, (T_q / 64 + n_seqs) * n_heads < 2^31.  A non-finite key or value reaches rows of its own
+ * T_q, T_k <= 2^31 - 2^10, row strides < 2^23, (T_q / 64 + n_seqs) * n_heads < 2^31.  A non-finite key or value reaches rows of its own
  * sequence only.
  */
 SR_API int sr_attn_prefill(const void *Q_f16, int64_t ldq, const void *K_f16, int64_t ldk, const void *V_f16, int64_t ldv,

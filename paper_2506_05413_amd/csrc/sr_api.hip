@@ -414,9 +414,10 @@ int sr_attn_prefill(const void *Q_f16, int64_t ldq, const void *K_f16, int64_t l
                     int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int causal, float scale,
                     void *O_f16, int64_t ldo, void *stream)
 {
-    constexpr int64_t most = ((int64_t)1 << 31) - 1, stride = 1 << 23;
+    // (tokens: the end of the tile that the last one lies in is counted in 32 bits too)
+    constexpr int64_t most = ((int64_t)1 << 31) - 1, tokens = most - 1023, stride = 1 << 23;
     if (!head_dim_ok(head_dim) || !scale_ok(scale)) return SR_ERR_ARG;
-    if (n_seqs < 0 || n_seqs >= most || T_q < 0 || T_q > most || T_k < 0 || T_k > most || !heads_fit(n_heads, n_kv_heads)) return SR_ERR_SHAPE;
+    if (n_seqs < 0 || n_seqs >= most || T_q < 0 || T_q > tokens || T_k < 0 || T_k > tokens || !heads_fit(n_heads, n_kv_heads)) return SR_ERR_SHAPE;
     if (ldq < n_heads * head_dim || ldo < n_heads * head_dim || ldk < n_kv_heads * head_dim || ldv < n_kv_heads * head_dim) return SR_ERR_SHAPE;
     if (ldq >= stride || ldk >= stride || ldv >= stride || ldo >= stride) return SR_ERR_SHAPE;
     if (sr::attn_prefill_workgroups(T_q, n_seqs, n_heads) > most) return SR_ERR_SHAPE;
