@@ -316,6 +316,7 @@ int sr_kv_quant_asym(const void *X_f16, int64_t rows, int64_t D, int64_t ldx, in
 
 // ---- paged cache and attention ----------------------------------------------------------------------------------------
 static bool head_dim_ok(int64_t d) { return d == 64 || d == 128; }
+static bool page_size_ok(int64_t n) { return sr::is_pow2(n) && n >= 16 && n <= (1 << 20); }
 
 static constexpr int64_t kMostHeads = 1 << 16;             // kernels divide rows by heads in fp32
 static constexpr float kLeastClip = 0x1p-64f;              // steps and their reciprocals stay normal numbers
@@ -324,7 +325,7 @@ static int check_cache(const sr_kv_cache *cache, sr::KvCache &c)
     if (!cache) return SR_ERR_NULL;
     if (cache->type != SR_KV_F16 && cache->type != SR_KV_I4) return SR_ERR_ARG;
     if (!head_dim_ok(cache->head_dim)) return SR_ERR_ARG;
-    if (!sr::is_pow2(cache->page_size) || cache->page_size < 16 || cache->page_size > (1 << 20)) return SR_ERR_ARG;
+    if (!page_size_ok(cache->page_size)) return SR_ERR_ARG;
     if (cache->n_pages < 1 || cache->n_pages >= ((int64_t)1 << 31) || cache->n_pages >= ((int64_t)1 << 40) / cache->page_size ||
         cache->n_kv_heads < 1 || cache->n_kv_heads >= kMostHeads)
         return SR_ERR_SHAPE;
@@ -381,7 +382,7 @@ int sr_kv_gather(const int64_t *slots, int64_t T, const sr_kv_cache *cache, void
 static bool decode_shape_ok(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t max_pages, int64_t page_size)
 {
     return n_seqs >= 0 && n_seqs < (1 << 20) && heads_fit(n_heads, n_kv_heads) && n_seqs * n_heads < (1 << 24) && max_pages >= 1 &&
-           page_size >= 16 && page_size <= (1 << 20) && max_pages <= (1 << 30) / page_size;
+           page_size_ok(page_size) && max_pages <= (1 << 30) / page_size;
 }
 
 size_t sr_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim, int64_t max_pages,
