@@ -8,8 +8,9 @@
  *
  * The conventions of smoothrot.h hold (device pointers, stream, statuses, no allocation, 16-byte aligned bases, row strides
  * multiples of 8 where the elements are fp16), but for shapes: head_dim is 64 or 128 (SR_ERR_ARG otherwise), any number of
- * tokens, sequences and heads (heads below 65536), n_heads a multiple of n_kv_heads (query head h reads key/value head
- * h / (n_heads / n_kv_heads)).  Rows of several heads lie one head after the other, [tokens, heads * head_dim].
+ * tokens, sequences and heads up to the limits given at each call (SR_ERR_SHAPE otherwise; heads below 65536), n_heads a multiple of
+ * n_kv_heads (query head h reads key/value head h / (n_heads / n_kv_heads)).  Rows of several heads lie one head after the other,
+ * [tokens, heads * head_dim].
  */
 #ifndef SMOOTHROT_ATTENTION_H
 #define SMOOTHROT_ATTENTION_H
@@ -80,8 +81,8 @@ SR_API int sr_kv_gather(const int64_t *slots, int64_t T, const sr_kv_cache *cach
 /*
  * Attention of one new token per sequence over its pages:
  *     o = sum_t p_t v_t,  p = softmax(scale * q . k_t)  over the tokens t < seq_lens[b]
- * with the values that the cache stands for (4 bits: (code - z) * d, not rounded); scores, maxima and sums in fp32, weights
- * rounded to fp16 for the product with the values, o rounded once.  The tokens of all sequences are dealt out in equal shares and
+ * with the values that the cache stands for (4 bits: (code - z) * d, not rounded); scores, maxima and sums in fp32, weights (4 bits:
+ * p_t d) rounded to fp16 for the product with the values and divided by the sum of the p_t before it, o rounded once.  The tokens of all sequences are dealt out in equal shares and
  * the parts of a sequence joined, unless the table is narrow or the sequences many; the same call gives the same bits.
  *   Q_f16        fp16 [n_seqs, n_heads * head_dim], row stride ldq
  *   page_table   int32 [n_seqs, max_pages], row stride ld_table: page i holds tokens i * page_size .. of the sequence.  Entries
@@ -93,7 +94,9 @@ SR_API int sr_kv_gather(const int64_t *slots, int64_t T, const sr_kv_cache *cach
  *   workspace    sr_attn_decode_workspace_bytes(...) bytes on the device that is current, 256-byte aligned (may be NULL where
  *                that is 0).  Contents need no initialisation; calls that share one must not overlap (captured graphs included).
  * Lengths are not known on the host: whether there are shares (and a workspace) follows n_seqs, the heads, the cache's type and
- * max_pages * page_size, so a table that is no wider than the longest sequence needs is best.  max_pages * page_size <= 2^30.
+ * max_pages * page_size, so a table that is no wider than the longest sequence needs is best.  From 1025 sequences, or 8 pairs of
+ * sequence and key/value head per compute unit, on there are no shares: a very long sequence is then better passed in a call of its own.
+ * max_pages * page_size <= 2^30, n_seqs < 2^20, n_seqs * n_heads < 2^24.
  *   type         of the cache: SR_KV_F16 or SR_KV_I4.  0 for arguments that sr_attn_decode refuses.
  */
 SR_API size_t sr_attn_decode_workspace_bytes(int64_t n_seqs, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim,

@@ -302,7 +302,7 @@ def sr_attn_decode(Q, cache, page_table, seq_lens, scale=None, O=None, workspace
 
 def sr_attn_prefill(Q, K, V, cu_q, cu_k, head_dim: int, causal: bool = True, scale=None, O=None):
     """Q fp16 [T_q, n_heads * head_dim], K, V fp16 [T_k, n_kv_heads * head_dim], cu_q, cu_k int32 [n_seqs + 1] -> O fp16 like Q.
-    scale: 1 / sqrt(head_dim) if None."""
+    scale: 1 / sqrt(head_dim) if None.  Rows of no sequence are not written: of an O that is made here they are uninitialised."""
     out = (_native or _marshal()).attn_prefill(Q, K, V, cu_q, cu_k, head_dim, causal, scale, O)
     return _refused(out, "sr_attn_prefill") if type(out) is int else out
 
