@@ -3,10 +3,11 @@
 //   s_t = scale q . k_t,   o = sum_t softmax(s)_t v_t     over the tokens t < length whose page exists
 //
 // Bound by the bytes of the cache where it is long (4 bits, 8 key/value heads of 128: 64 sequences of 0 .. 8192 tokens, 294 MB, in
-// 55 us = 5.3 TB/s; fp16, 32 heads of 64: 24 sequences of 2000 tokens, 241 MB, in 45 us), else by the launch and the chain of
-// loads and tiles of one sequence (130 tokens 5.6 us, 0.8 us for a wave's tile; 65000 tokens, 75 MB, 21 us with the join).  A workgroup
+// 55 us = 5.3 TB/s; fp16, 32 heads of 64: 24 sequences of 0 .. 2000 tokens, 239 MB, in 45 us), else by the launch and the chain of
+// loads and tiles of one sequence (130 tokens 5.5 us, 0.7 us for a wave's tile; 65000 tokens, 75 MB, 21 us with the join).  A workgroup
 // takes one key/value head (up to 16 of the query heads that share it) and runs of tokens; its waves walk over tiles of 32 tokens
-// with a running maximum and sum, and meet in LDS.  Both products run on 16 x 16 x 32 matrix instructions with the query head in
+// with a running maximum and sum, and meet in LDS.  (More query heads to a key/value head are workgroups of their own, each of which
+// asks for the cache again: 64 sequences of 0 .. 8192 tokens, 37 MB, 16 query heads on one key/value head 20.5 us, 32 26.9.)  Both products run on 16 x 16 x 32 matrix instructions with the query head in
 // the columns:
 //
 //   S^T = K Q^T   rows = tokens: lane (n, g) = (lane % 16, lane / 16) holds token n of the operand and gets tokens 4 g + r
@@ -15,8 +16,8 @@
 //
 // Where up to 4 (8) query heads share a key/value head, the sixteen columns hold 4 (2) copies of them (4 bits), and a copy forms the
 // weights of every fourth (of every other pair of) token only, zeros for the rest, so that no lane forms a weight that another has
-// too; the copies' sums are added up at the end (64 sequences of 0 .. 8192 tokens 57.2 -> 55.4 us, 16 of 2000 14.8 -> 13.6, 200 of up
-// to 500 21.2 -> 19.4).
+// too; the copies' sums are added up at the end (64 sequences of 0 .. 8192 tokens 57.3 -> 55.3 us, 16 of 2000 14.7 -> 13.5, 200 of up
+// to 500 20.7 -> 18.9).
 //
 // The order of channels in the first product and of columns in the second is free, so both operands are taken as they lie in
 // memory, and the sums over codes need no conversion: a code c in bits 4-7 of a half is the subnormal fp16 number c 2^-20, a
@@ -26,8 +27,11 @@
 //   s_t = d (q . c - z sum(q)),   o = sum_t w_t (c_t - z_t),   w_t = p_t d_t
 // where p = 2^(s log2(e) - top - lift), top the maximum of the scores and lift that of the tokens' (score - top) + log2(d): weights
 // w then are at most 2^8 however large or small the values are, and lose nothing to the range of fp16.  (One sum of the two would
-// not do: beside a score of 2^28 it has no room for the other.)  w is rounded to fp16 for the matrix pipe (half a step, 2^-11 of it; the
-// same rounded w multiplies z), sums and maxima are fp32.
+// not do: beside a score of 2^28 it has no room for the other.)  Scores, p, maxima and sums are fp32.  w is rounded to fp16, the type of
+// the matrix pipe's operands (half a step, 2^-11 of it; the same rounded w multiplies z): what that leaves would be another operand
+// and a second product for every tile, and is less than the rounding of the output (rms distance from 64 bits over normal values
+// 2.3e-4 of them, and 2.1e-4 without it).  The denominator is the sum of p as it is: at 4 bits w is p times the token's step, and the sum of
+// the rounded w is none of the rounded p.  (Prompts have fp16 values, hence w = p, and divide by the sum of the rounded ones.)
 #include "gemm_common.h"
 
 namespace sr {
@@ -69,8 +73,8 @@ struct Decode {
 // [w, w + 1) * size of it: pieces of several sequences, or a piece of one.  Sizes follow from the lengths, which are known on
 // the device only, so every wave adds them up itself.  A sequence inside one share is finished there; else the share in which
 // it begins leaves a partial result in place 1, the others leave theirs in place 0, and the second kernel joins them.
-// (64 sequences of 0 .. 8192 tokens, 8 key/value heads of 128, 4 bits, 294 MB: the shares take 56 us, and cutting every sequence
-// into 2, 4 or 8 runs 74 - 77.)
+// (64 sequences of 0 .. 8192 tokens, 8 key/value heads of 128, 4 bits, 294 MB: cutting every sequence into 2, 4 or 8 runs took 1.3
+// times as long as the shares, with an earlier form of the tiles.)
 __device__ __forceinline__ int length_of(const Decode &a, int b) { return (int)min((int64_t)max(a.lens[b], 0), a.max_len); }
 __device__ __forceinline__ int rounds_of(const Decode &a, int b) { return b < a.n_seqs ? (length_of(a, b) + kRound - 1) / kRound : 0; }
 
@@ -154,7 +158,7 @@ template <int D> struct Stage {
 };
 
 // 16 bytes per lane from addresses of its own to LDS bytes [lds, lds + 1024), in the order of the lanes.  The cache is read once:
-// with loads that allocate in the caches 64 sequences of 4096 tokens (302 MB) took 77 us, with these 64.
+// with loads that allocate in the caches 64 sequences of 4096 tokens (303 MB) take 60.7 us, with these 53.5.
 __device__ __forceinline__ void dma16_once(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(lds), "v"(p) : "memory", "m0");
@@ -656,9 +660,9 @@ template <int D, bool I4, int COPIES, int WAVES> hipError_t launch_waves(const D
     return hipGetLastError();
 }
 
-// Eight waves where a workgroup has a unit to itself and a whole sequence to do (4 bits; us, 4 waves / 8: one sequence of 500 tokens 7.6
-// / 7.1, 16 of 2000 17.5 / 14.3, 32 of up to 2000 17.8 / 14.8; 64 of 500 10.2 / 13.0.  Sixteen 9.4, 17.7, 20.2 and 21.  fp16 gains nothing:
-// 32 of 1000 19.6 / 19.4).
+// Eight waves where a workgroup has a unit to itself and a whole sequence to do (4 bits; us, 4 waves / 8: one sequence of 500 tokens 7.1
+// / 7.0, of 1000 9.9 / 9.0, 16 of 2000 16.2 / 13.6, 32 of up to 2000 16.1 / 13.6; 64 of 500 11.3 / 11.9, 200 of up to 500 18.9 / 24.6.  Sixteen
+// were slower than eight everywhere, and fp16 gained nothing, 32 of 1000, when that was measured on an earlier form of the kernel).
 template <int D, bool I4, int COPIES> hipError_t launch_copies(const Decode &a, hipStream_t st)
 {
     if constexpr (I4)
@@ -685,12 +689,16 @@ template <int D> hipError_t launch_join(const Decode &a, hipStream_t st)
 }
 
 // Shares of the sequences of one key/value head and row tile; 0: a workgroup per sequence does it all, which needs no second
-// kernel (4 us) and no change from one sequence to the next, but takes as long as the longest sequence: 0.8 us a round (4 bits; with
-// eight waves 0.75; fp16, which keeps one tile of a wave on its way, 1.6), or what the bytes take.  Measured (us, shares / a workgroup each):
-//   4 bits, 8 key/value heads of 128:  1 sequence of 500 tokens 8.7 / 7.1, 896 8.8 / 8.5, 1000 9.2 / 9.4;  8 of 1000 10.6 / 9.7, 1300
-//     14.0 / 11.1, up to 2000 12.9 / 14.0;  16 of 2000 17.8 / 14.7, up to 3000 19.7 / 18.7, 4000 21.1 / 22.9;  32 of up to 3000 22.1 / 19.6,
-//     4000 24.1 / 24.0;  64 of up to 2000 26.6 / 23.0, 8192 56 / 95;  128 of up to 2000 45 / 37, 4096 60 / 67
-//   fp16:  1 of 384 8.7 / 7.2;  8 of 500 10.2 / 11.2;  32 of 500 17.4 / 13.5;  64 of up to 1000 30.5 / 33.5
+// kernel (4 us) and no change from one sequence to the next, but takes as long as the longest sequence: 0.7 us a round (4 bits; with
+// eight waves 0.5 for as many tokens; fp16, which keeps one tile of a wave on its way, 1.4), or what the bytes take.  Measured (us,
+// shares / a workgroup each; * where the rule takes the slower one):
+//   4 bits, 8 key/value heads of 128:  1 sequence of 500 tokens 8.8 / 7.0, 896 8.9 / 8.3, 1000 9.1 / 9.0;  8 of 1000 10.8 / 9.4, 1300
+//     14.1 / 10.6, up to 2000 10.7 / 13.0;  16 of 2000 14.5 / 13.6, up to 3000 15.8 / 16.9 *, 4000 19.1 / 20.6;  32 of up to 3000 21.6 / 17.5,
+//     4000 24.9 / 21.2 *;  64 of up to 2000 27.0 / 19.5, 8192 55.0 / 65.3;  128 of up to 2000 37.8 / 32.7, 4096 62.2 / 64.1
+//   fp16:  1 of 384 8.7 / 7.8;  8 of 500 10.4 / 11.2;  32 of 500 19.7 / 15.7, 1000 28.3 / 24.6 *;  64 of up to 1000 27.2 / 30.9
+// The rule goes by counts, since lengths are not known here.  Where there are no shares for the number of sequences, one long
+// sequence among many short ones is a workgroup's for each of its heads: 65000 tokens beside 254 sequences of up to 300 take 60 us, beside
+// 255 of them, eight pairs to a unit, 359.
 int shares_of(int64_t n_seqs, int64_t per_seq, int64_t max_len, bool i4)
 {
     const int64_t units = compute_units(), rounds = (max_len + kRound - 1) / kRound, shares = 2 * units / per_seq;

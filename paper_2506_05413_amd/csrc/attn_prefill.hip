@@ -17,18 +17,20 @@
 // weight might pass 2^16: the sum of a tile's weights, which is needed anyhow, shows it, so that a tile needs no maximum, and most
 // tiles rescale nothing.  The products of a tile are summed up from -top on, so that a difference is rounded as the score is,
 // however large.  Weights are rounded to fp16 for the matrix pipe (half a step, 2^-11 of each; subnormal below 2^-21 of the
-// largest at least), and the sum in the denominator is that of the rounded ones.  Scores, sums and outputs are held in fp32.
+// largest at least), and the sum in the denominator is that of the rounded ones, so that equal values come out as they are.  (The
+// rest of a weight would be another operand and a second product for every tile; the outputs' own rounding is as large: rms distance
+// from 64 bits over normal values 2.3e-4 of them, and 2.0e-4 without it.)  Scores, sums and outputs are held in fp32.
 //
 // What bounds it: long prompts the power the chip may draw (8192 tokens, 32 heads of 128, causal: the clock is 1.83 GHz of 2.4 and
 // the matrix pipe busy for half of the cycles), the others the chain of a row's tiles.  Per 64 keys and SIMD, two waves there, the
 // products alone take 0.85 us, with the weights 1.05, with the reads from LDS 1.3; one wave takes 1.05.  Hence four shapes of
 // workgroup (us; 32 and 8 heads of 128, causal, one prompt of T tokens; 8 and 8 heads; nine prompts of T tokens together):
 //                                               T = 512   1024   2048   4096   8192  |  3000   4096   6000  |   400   1000
-//   8 row waves  a tile loaded once for 256        17.2   29.5   57.5    138    515  |    69     93    134  |   7.3   14.7
-//   4 row waves  two workgroups on a unit          13.0   22.8   46.2    145         |    51     70    108  |   6.7   12.3
-//   2 x 2 sets   the sets take every other tile    10.7   22.1   60.9    200         |    37     55    114  |  10.7   18.2
+//   8 row waves  a tile loaded once for 256        17.7   31.2   58.4    139    518  |    70     95    134  |   7.6   10.9
+//   4 row waves  two workgroups on a unit          13.4   23.9   48.0    147    535  |    52     70    108  |   6.4   10.0
+//   2 x 2 sets   the sets take every other tile    11.1   23.3   64.3    202    752  |    37     55    114  |  11.7   18.5
 //                and meet in LDS at the end
-//   2 x 4 sets   tiles of 32 keys                  10.8   21.7   58.5    192         |    33     51    107  |  11.2   19.0
+//   2 x 4 sets   tiles of 32 keys                  11.2   23.0   62.1    193    718  |    33     51    106  |  11.7   19.3
 // Products interleaved with the weights of the tile before (three tiles in flight) were 9 % slower at 8192 tokens and 15 % at
 // 1024, 64 rows per wave (one wave per SIMD) 30 % slower, and two halves of a workgroup that multiply and weigh in turn, by
 // barriers, 6 .. 30 % slower.

@@ -7,8 +7,8 @@
 // Every product, sum and quotient comes out as rounded on its own: keys are rounded to fp16 and values next to a rounding
 // boundary take the code that the formula in fp32 gives, whoever evaluates it.
 //
-// Bound by its bytes where there are many tokens (16384 with 32 query heads and 8 key/value heads of 128, 4 bits: 387 MB in 75 us,
-// 5.1 TB/s; 2047 with the transform 13 us, 3.7 TB/s), else by the launch (one token 2.3 us).  Eight values (16 bytes) per lane,
+// Bound by its bytes where there are many tokens (16384 with 32 query heads and 8 key/value heads of 128, 4 bits: 387 MB in 76 us,
+// 5.1 TB/s; 2047 with the transform 13.2 us, 3.7 TB/s), else by the launch (one token 2.7 us).  Eight values (16 bytes) per lane,
 // D / 8 lanes per row, a row being one head of one token, query, key or value; the head's other half, the butterflies and the
 // range of a row are exchanged between those lanes with operand permutations, without LDS.
 #include "sr_common.h"
@@ -187,10 +187,11 @@ struct Append {
 };
 
 // APART: a wave's rows are all queries, all keys or all values, so that what differs between those is scalar; else rows lie in the
-// order of the tokens.  Measured (us, apart / in order; 32 + 2 x 8 heads of 128): with the transform 1024 tokens 8.3 / 9.3, 2047
-// 13.0 / 13.8, 4096 23.5 / 24.9, 16384 95 / 95; without it 2047 10.6 / 11.2, 4096 19.6 / 20.4, 8192 41.4 / 41.4 (fp16 42.7 / 40.7),
-// 16384 79 / 75 (fp16 82 / 75).
-// (One row per group of lanes: two or four, on their way together, were 2 - 8 % slower up to 4096 tokens and 4 % faster at 16384.)
+// order of the tokens.  Measured (us, apart / in order; 32 + 2 x 8 heads of 128): with the transform 1024 tokens 8.5 / 9.2, 2047
+// 13.3 / 13.4, 4096 24.3 / 24.6, 16384 95.6 / 93.7; without it 2047 10.7 / 11.1, 4096 19.9 / 20.4, 8192 42.0 / 40.7 (fp16 43.2 / 41.0),
+// 16384 80.1 / 76.1 (fp16 83.2 / 75.8).
+// (One row per group of lanes: two or four, on their way together, were 2 - 8 % slower up to 4096 tokens and 4 % faster at 16384, before
+// waves were told apart.)
 template <int D, bool I4, bool PAIRS, bool HAD, bool APART> __global__ __launch_bounds__(256) void rope_kv_append_kernel(Append a)
 {
     constexpr int LPR = D / 8, ROWS = 64 / LPR;          // rows of a wave
@@ -318,8 +319,8 @@ template <int D, bool I4, int N> __global__ __launch_bounds__(256) void kv_gathe
     }
 }
 
-// Two rows per group of lanes from eight workgroups on every compute unit on (16384 tokens of 8 heads of 128, 4 bits: 21.9 ->
-// 19.8 us, 86 MB; four 19.3, but 4096 tokens 6.3 -> 6.7); nothing gained or lost below.
+// Two rows per group of lanes from eight workgroups on every compute unit on (16384 tokens of 8 heads of 128, 4 bits, 86 MB: 20.4 ->
+// 18.5 us, 4096 7.0 -> 6.3; fp16, 134 MB, 28.0 -> 26.7); little gained or lost below (2047 tokens 4.17 -> 4.10).
 template <int D, bool I4> hipError_t gather_dim(const Gather &a, hipStream_t st)
 {
     constexpr unsigned rows = 256 / (D / 8);
